@@ -354,7 +354,7 @@ def _own(s):
         d = B.norm_desc(rows, ch, c["stream"], c["branch"], EPS, c["fmt"], ld_stream=ch + pad, ld_branch=ch + pad)
         if op == "norm_fwd":
             B.revnet_rmsnorm_fwd(ctx, d, s["x"], s["r"], s["gamma"], s["h"], s["n"], s["ck"], s["rstd"])
-            B.revnet_act8_load(ctx, B.act8_desc(rows, ch, "bf16", c["fmt"]), s["ck"], s["kept"])
+            B.revnet_act_load(ctx, B.act_desc(rows, ch, "bf16", c["fmt"]), s["ck"], s["kept"])
             out = dict(n=s["n"], rstd=s["rstd"], kept=s["kept"])
             return dict(out, h=s["h"]) if s["r"] is not None else out
         if "ws" not in s:
@@ -364,19 +364,19 @@ def _own(s):
     if op.startswith("act"):
         ch = c["channels"]
         out = ch // 2 if c["act"] == "swiglu" else ch
-        d = B.act8_desc(rows, ch, c["dtype"], c["fmt"], c["act"], ld_x=ch + pad, ld_a=out + pad)
+        d = B.act_desc(rows, ch, c["dtype"], c["fmt"], c["act"], ld_x=ch + pad, ld_a=out + pad)
         if op == "act_fwd":
-            B.revnet_act8_store(ctx, d, s["x"], s["ck"], s["a"])
-            B.revnet_act8_load(ctx, B.act8_desc(rows, ch, "bf16", c["fmt"]), s["ck"], s["kept"])
+            B.revnet_act_store(ctx, d, s["x"], s["ck"], s["a"])
+            B.revnet_act_load(ctx, B.act_desc(rows, ch, "bf16", c["fmt"]), s["ck"], s["kept"])
             return dict(a=s["a"], kept=s["kept"])
-        B.revnet_act8_bwd(ctx, d, s["ck"], s["da"], s["dx"], s["a_ck"])
-        B.revnet_act8_load(ctx, B.act8_desc(rows, out, "bf16", c["fmt"]), s["a_ck"], s["kept"])
+        B.revnet_act_bwd(ctx, d, s["ck"], s["da"], s["dx"], s["a_ck"])
+        B.revnet_act_load(ctx, B.act_desc(rows, out, "bf16", c["fmt"]), s["a_ck"], s["kept"])
         return dict(dx=s["dx"], kept=s["kept"])
     if op == "wgrad":
-        d = B.wgrad8_desc(rows, c["cin"], c["cout"], c["dtype"], c["fmt"], ld_dy=c["cout"] + pad)
+        d = B.wgrad_desc(rows, c["cin"], c["cout"], c["dtype"], c["fmt"], ld_dy=c["cout"] + pad)
         if "ws" not in s:
-            s["ws"] = torch.empty(B.revnet_wgrad8_workspace_bytes(ctx, d), dtype=torch.uint8, device="cuda")
-        B.revnet_wgrad8(ctx, d, s["dy"], s["ck"], s["gamma"], s["dW"], s["ws"])
+            s["ws"] = torch.empty(B.revnet_linear_wgrad_workspace_bytes(ctx, d), dtype=torch.uint8, device="cuda")
+        B.revnet_linear_wgrad(ctx, d, s["dy"], s["ck"], s["gamma"], s["dW"], s["ws"])
         return s["dW"]
     d = B.logprob_desc(rows, c["vocab"], c["dtype"], min(c["k"], c["vocab"]), ld=c["vocab"] + pad)
     if op == "logp_fwd":
