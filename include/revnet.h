@@ -299,6 +299,120 @@ int revnet_train_step_host(revnet_ctx *ctx, revnet_plan *plan,
                            float *loss_host, int32_t *pred_host,
                            revnet_step_stats *stats, void *stream);
 
+/* ---- operators on rows of tokens ----
+ * A residual function over tokens (rows of `channels` values, the pixels of an NHWC tensor among them) in place of images: a
+ * root-mean-square norm instead of BN, linear layers instead of convolutions, a loss over a vocabulary.  What such a function keeps for
+ * its backward pass is kept in 8 bits (the paper's Section 3.2 recomputes it; these are the layers that cannot be).
+ *
+ * Conventions beyond those above
+ *   - Rows are `ld` elements apart, channels contiguous; ld = 0 stands for the row's length.  Rows of 16-byte multiples at 16-byte
+ *     addresses take wide accesses; any other stride, length or (element-aligned) address is legal and slower.
+ *   - rows = 0 is legal: nothing is read, row outputs stay as they are, gradients of parameters are set to zero.  Row tensors may then be null.
+ *   - Elements between a row's end and the next row's start, and rows behind the last one, are neither read nor written.
+ *   - float32 arithmetic on every type; bf16 outputs are rounded once, at the end.
+ *   - The context's device must be the current one.  Results do not depend on timing: no sum is formed by atomics.
+ *   - Outputs may alias inputs only where a call says so. */
+typedef enum { REVNET_F32 = 0, REVNET_BF16 = 1 } revnet_dtype;
+typedef enum { REVNET_INT8 = 0, REVNET_E4M3 = 1 } revnet_code;
+typedef enum {
+    REVNET_ACT_NONE = 0,
+    REVNET_ACT_RELU = 1,
+    REVNET_ACT_GELU = 2,               /* x / (1 + exp(-2 sqrt(2/pi) (x + 0.044715 x^3))), the tanh form */
+    REVNET_ACT_SILU = 3,               /* x / (1 + exp(-x)) */
+    REVNET_ACT_SWIGLU = 4              /* rows x = [g | u] of two halves, a = silu(g) * u: half as many channels */
+} revnet_act;
+
+/* An 8-bit checkpoint of a [rows][channels] tensor, one caller-owned buffer (256-byte aligned):
+ *   codes   [rows][pitch] bytes, pitch = channels rounded up to 32; int8, or e4m3 (OCP 8-bit floating point); 0 behind the last channel
+ *   scales  [ceil(channels / 128)][rows rounded up to 64][4] bytes, at the next multiple of 256 bytes: byte b of row r and of
+ *           channels 32 j .. 32 j + 31 is at [j / 4][r][j % 4] and stands for 2^(b - 127)
+ * A value is code * scale.  The scale is the smallest power of two (not below 2^-117) with which the block's largest magnitude fits
+ * into 127 (int8) or 448 (e4m3); codes are rounded to nearest, ties to even.  So nothing is clipped, the error is at most half a
+ * step of the code, and every value held is exactly a bf16 number: a product on the bf16 tensor cores takes just what is held.  A block
+ * with an infinity or a NaN has b = 255 and codes 0, and all of it reads back as NaN.  Scale bytes of rows behind the last one and of
+ * blocks behind the last channel are not written. */
+int revnet_act_ckpt_bytes(revnet_ctx *ctx, int64_t rows, int channels, size_t *bytes);
+
+typedef struct {
+    int64_t rows;            /* rows * pitch < 2^35 */
+    int channels;            /* of x; 1 .. 2^20; even with REVNET_ACT_SWIGLU */
+    int dtype;               /* revnet_dtype of x and a (dx and da) */
+    int code;                /* revnet_code of the checkpoint */
+    int act;                 /* revnet_act */
+    int64_t ld_x, ld_a;      /* row strides of x (dx) and of a (da) */
+} revnet_act_desc;
+/* ck = checkpoint of x, a = act(x) (from x itself, not from its checkpoint).  a may be null; without REVNET_ACT_SWIGLU a == x is legal. */
+int revnet_act_store(revnet_ctx *ctx, const revnet_act_desc *desc, const void *x, void *ck, void *a, void *stream);
+/* a = act(x8), x8 what the checkpoint holds (REVNET_ACT_NONE: x8 itself). */
+int revnet_act_load(revnet_ctx *ctx, const revnet_act_desc *desc, const void *ck, void *a, void *stream);
+/* dx = da * act'(x8) (ReLU'(0) = 0).  a_ck (may be null): checkpoint of act(x8) in the same code, the operand of the next layer's
+ * weight gradient.  Without REVNET_ACT_SWIGLU dx == da is legal. */
+int revnet_act_bwd(revnet_ctx *ctx, const revnet_act_desc *desc, const void *ck, const void *da, void *dx, void *a_ck, void *stream);
+
+/* Root-mean-square norm behind the residual's addition (the coupling y = x + F of Section 3.1, then the next function's norm):
+ *   h = x + r rounded to the stream's type, rstd = 1 / sqrt(mean(h^2) + eps), xh = h * rstd, n = xh * gamma. */
+typedef struct {
+    int64_t rows;            /* < 2^31 */
+    int channels;            /* 1 .. 16384 */
+    int stream_dtype;        /* of x, h, dh, dx: the residual stream */
+    int branch_dtype;        /* of r, n, dn, dr: the residual function; REVNET_F32 only with a REVNET_F32 stream */
+    int code;                /* revnet_code of ck */
+    int ck_scaled;           /* 1: ck holds n (the operand of an 8-bit product); 0: ck holds xh (what revnet_rmsnorm_bwd reads) */
+    float eps;               /* > 0 */
+    int64_t ld_stream, ld_branch;
+} revnet_norm_desc;
+/* r null: h = x (h must then be null).  gamma ([channels] float32) null: ones.  h, n, ck and rstd ([rows] float32) may each be null.
+ * h == x is legal. */
+int revnet_rmsnorm_fwd(revnet_ctx *ctx, const revnet_norm_desc *desc, const void *x, const void *r, const float *gamma,
+                       void *h, void *n, void *ck, float *rstd, void *stream);
+/* Workspace of the backward call: per-CTA sums of dgamma. */
+int revnet_rmsnorm_workspace_bytes(revnet_ctx *ctx, const revnet_norm_desc *desc, size_t *bwd_bytes);
+/* dx = dh + rstd (gamma dn - xh mean(gamma dn xh)), dgamma = sum over rows of dn xh.
+ * Either h is given (ck and rstd null: rstd is formed again) or ck with ck_scaled = 0 and rstd are (h null).
+ * dh (the gradient that reaches h past the norm) may be null; dr (dx once more, in the branch's type: the gradient of r) and dgamma
+ * may be null.  dx == dh is legal. */
+int revnet_rmsnorm_bwd(revnet_ctx *ctx, const revnet_norm_desc *desc, const void *dn, const void *dh, const void *h, const void *ck,
+                       const float *rstd, const float *gamma, void *dx, void *dr, float *dgamma,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* Weight gradient of a linear layer (a 1x1 convolution) whose input was kept in 8 bits:
+ *   dW[o][c] = gamma[c] * sum over rows t of dy[t][o] * x8[t][c],   dW [cout][cin] float32, overwritten
+ * on the tensor cores.  Products are exact: x8 and a bf16 dy are bf16 operands; a float32 dy is split into three bf16 numbers that
+ * together hold all its 24 bits (three products).  gamma null: ones. */
+typedef struct {
+    int64_t rows;            /* < 2^29 */
+    int cin, cout;           /* 1 .. 65536 */
+    int dy_dtype;            /* revnet_dtype */
+    int code;                /* revnet_code of ck */
+    int64_t ld_dy;
+} revnet_wgrad_desc;
+int revnet_linear_wgrad_workspace_bytes(revnet_ctx *ctx, const revnet_wgrad_desc *desc, size_t *bytes);
+int revnet_linear_wgrad(revnet_ctx *ctx, const revnet_wgrad_desc *desc, const void *dy, const void *ck, const float *gamma, float *dW,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens (the head's softmax cross-entropy for large vocabularies): per row of logits x
+ *   lse = log sum exp(x_j), logp = x_target - lse, entropy = -sum p_j log p_j (0 log 0 = 0), p_j = exp(x_j - lse),
+ *   and the k most likely tokens, the lowest index first among equals, with their log probabilities.
+ * target -1: a row without a target, logp = 0.  Another target outside [0, vocab): logp = NaN, and the device status becomes
+ * REVNET_E_INVALID_ARG (see revnet_check_device).  -inf logits have probability 0; a row of nothing else has lse = logp = -inf and
+ * entropy 0, and its most likely tokens are 0 .. k - 1 with -inf.  A row with a NaN or +inf has NaN for lse, logp and entropy; its
+ * most likely tokens are ordered by the logits, NaN first. */
+typedef struct {
+    int64_t rows;            /* < 2^31 */
+    int vocab;               /* 1 .. 2^24 */
+    int dtype;               /* revnet_dtype of the logits and their gradient */
+    int k;                   /* 0 .. min(32, vocab) */
+    int64_t ld;
+} revnet_logprob_desc;
+/* targets [rows] int32.  logp (with targets), entropy, lse: [rows] float32, each may be null; top_logp, top_index: [rows][k], both or (k = 0) neither. */
+int revnet_logprobs_fwd(revnet_ctx *ctx, const revnet_logprob_desc *desc, const void *logits, const int32_t *targets,
+                        float *logp, float *entropy, float *lse, float *top_logp, int32_t *top_index, void *stream);
+/* dlogits_j = dlogp (1[j = target] - p_j) - dentropy p_j (log p_j + entropy), 0 where p_j = 0 and j is not the target.
+ * dlogp (with targets) or dentropy (with entropy) may be null: 0.  dlogits == logits is legal.  A target outside [-1, vocab) makes its
+ * row NaN (where p > 0) and sets the device status.  A row whose lse is -inf gets zeros. */
+int revnet_logprobs_bwd(revnet_ctx *ctx, const revnet_logprob_desc *desc, const void *logits, const int32_t *targets,
+                        const float *lse, const float *entropy, const float *dlogp, const float *dentropy, void *dlogits, void *stream);
+
 /* Waits inside the library's kernels (on shared-memory barriers) are bounded; a kernel whose wait
  * runs out stops its work, records a status word on the device and exits normally.  The loss kernel
  * records REVNET_E_INVALID_ARG the same way when a label lies outside [0, n_classes) (it reads

@@ -24,7 +24,10 @@ EXPORTS = ["revnet_create", "revnet_destroy", "revnet_last_error", "revnet_block
            "revnet_train_step", "revnet_train_step_host", "revnet_profile_enable", "revnet_profile_summary", "revnet_check_device", "revnet_plan_scratch_split",
            "revnet_transition_workspace_bytes", "revnet_transition_fwd", "revnet_transition_bwd",
            "revnet_block_fwd_noalloc", "revnet_block_pack_bytes", "revnet_pack_weights", "revnet_selftest_bounded_wait",
-           "revnet_plan_set_buffer_sizes"]
+           "revnet_plan_set_buffer_sizes",
+           "revnet_act_ckpt_bytes", "revnet_act_store", "revnet_act_load", "revnet_act_bwd",
+           "revnet_rmsnorm_fwd", "revnet_rmsnorm_workspace_bytes", "revnet_rmsnorm_bwd",
+           "revnet_linear_wgrad_workspace_bytes", "revnet_linear_wgrad", "revnet_logprobs_fwd", "revnet_logprobs_bwd"]
 
 
 class FnDesc(C.Structure):
@@ -69,6 +72,24 @@ class StepStats(C.Structure):
                 ("recon_max_abs", C.c_float * MAX_STAGES), ("device_status", C.c_int)]
 
 
+class ActDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("channels", C.c_int), ("dtype", C.c_int), ("code", C.c_int), ("act", C.c_int),
+                ("ld_x", C.c_int64), ("ld_a", C.c_int64)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("channels", C.c_int), ("stream_dtype", C.c_int), ("branch_dtype", C.c_int), ("code", C.c_int),
+                ("ck_scaled", C.c_int), ("eps", C.c_float), ("ld_stream", C.c_int64), ("ld_branch", C.c_int64)]
+
+
+class WgradDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cin", C.c_int), ("cout", C.c_int), ("dy_dtype", C.c_int), ("code", C.c_int), ("ld_dy", C.c_int64)]
+
+
+class LogprobDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int), ("dtype", C.c_int), ("k", C.c_int), ("ld", C.c_int64)]
+
+
 def lib():
     """Load the CUDA library; there is no fallback if it is missing."""
     global _lib
@@ -105,6 +126,7 @@ def _stream():
 class Context:
     def __init__(self, device: int = 0):
         self.h = C.c_void_p()
+        self.device = device
         rc = lib().revnet_create(C.byref(self.h), C.c_int(device))
         if rc:
             raise RevnetError(f"revnet_create failed ({rc})")
@@ -372,3 +394,170 @@ def revnet_block_fwd_noalloc(ctx, desc, x1, x2, F, G, y1, y2):
     fp, gp = _fn_params(F), _fn_params(G)
     ctx.check(lib().revnet_block_fwd_noalloc(ctx.h, C.byref(desc), _ptr(x1), _ptr(x2), C.byref(fp), C.byref(gp),
                                              _ptr(y1), _ptr(y2), _stream()), "revnet_block_fwd_noalloc")
+
+
+# ------------------------------------------------------------------ operators on rows of tokens
+# Tensors are checked against their descriptor before their addresses are handed on: type, device, number of elements and row stride.
+# A row tensor is any view whose channels are contiguous; its rows are the descriptor's row stride apart.
+DTYPE = {"f32": 0, "bf16": 1}
+CODE = {"int8": 0, "e4m3": 1}
+ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
+_TYPE_NAMES = ("torch.float32", "torch.bfloat16")
+
+
+def act_desc(rows, channels, dtype="bf16", code="int8", act="none", ld_x=0, ld_a=0) -> ActDesc:
+    return ActDesc(rows, channels, DTYPE[dtype], CODE[code], ACT[act], ld_x, ld_a)
+
+
+def norm_desc(rows, channels, stream="f32", branch="bf16", eps=1e-5, code="int8", ck_scaled=False, ld_stream=0, ld_branch=0) -> NormDesc:
+    return NormDesc(rows, channels, DTYPE[stream], DTYPE[branch], CODE[code], int(ck_scaled), eps, ld_stream, ld_branch)
+
+
+def wgrad_desc(rows, cin, cout, dtype="bf16", code="int8", ld_dy=0) -> WgradDesc:
+    return WgradDesc(rows, cin, cout, DTYPE[dtype], CODE[code], ld_dy)
+
+
+def logprob_desc(rows, vocab, dtype="bf16", k=0, ld=0) -> LogprobDesc:
+    return LogprobDesc(rows, vocab, DTYPE[dtype], k, ld)
+
+
+def _bad(what, name, why):
+    e = RevnetError(f"{what}: {name} {why}")
+    e.status = -1
+    raise e
+
+
+def _row_ptr(ctx, what, name, t, rows, channels, ld, dtype):
+    """Address of a [rows][channels] tensor (None: null)."""
+    if t is None:
+        return None
+    if str(t.dtype) != _TYPE_NAMES[dtype] or t.device.type != "cuda" or t.device.index != ctx.device:
+        _bad(what, name, f"must be {_TYPE_NAMES[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if tuple(t.shape) != (rows, channels) or (channels > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or channels)):
+        _bad(what, name, f"must be [{rows}][{channels}] with rows {ld or channels} elements apart, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _flat_ptr(ctx, what, name, t, n, dtype="torch.float32"):
+    """Address of n contiguous elements, or of at least n bytes (None: null)."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype or t.device.type != "cuda" or t.device.index != ctx.device or not t.is_contiguous():
+        _bad(what, name, f"must be contiguous {dtype} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if t.numel() < n if dtype == "torch.uint8" else t.numel() != n:
+        _bad(what, name, f"must hold {n} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _ck_bytes(rows, channels):
+    pitch = (channels + 31) // 32 * 32
+    return (rows * pitch + 255) // 256 * 256 + (channels + 127) // 128 * ((rows + 63) // 64 * 64) * 4
+
+
+def _ck_ptr(ctx, what, name, t, rows, channels):
+    return _flat_ptr(ctx, what, name, t, _ck_bytes(rows, channels), "torch.uint8")
+
+
+def _stream_of(ctx):
+    import torch
+    return torch.cuda.current_stream(ctx.device).cuda_stream
+
+
+_P = C.c_void_p
+
+
+def revnet_act_ckpt_bytes(ctx, rows, channels) -> int:
+    n = C.c_size_t()
+    ctx.check(lib().revnet_act_ckpt_bytes(ctx.h, C.c_int64(rows), C.c_int(channels), C.byref(n)), "revnet_act_ckpt_bytes")
+    return n.value
+
+
+def _a_channels(desc):
+    return desc.channels // 2 if desc.act == ACT["swiglu"] else desc.channels
+
+
+def revnet_act_store(ctx, desc, x, ck, a=None):
+    w = "revnet_act_store"
+    px = _row_ptr(ctx, w, "x", x, desc.rows, desc.channels, desc.ld_x, desc.dtype)
+    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
+    pa = _row_ptr(ctx, w, "a", a, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
+    ctx.check(lib().revnet_act_store(ctx.h, C.byref(desc), _P(px), _P(pc), _P(pa), _P(_stream_of(ctx))), w)
+
+
+def revnet_act_load(ctx, desc, ck, a):
+    w = "revnet_act_load"
+    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
+    pa = _row_ptr(ctx, w, "a", a, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
+    ctx.check(lib().revnet_act_load(ctx.h, C.byref(desc), _P(pc), _P(pa), _P(_stream_of(ctx))), w)
+
+
+def revnet_act_bwd(ctx, desc, ck, da, dx, a_ck=None):
+    w = "revnet_act_bwd"
+    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
+    pda = _row_ptr(ctx, w, "da", da, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
+    pdx = _row_ptr(ctx, w, "dx", dx, desc.rows, desc.channels, desc.ld_x, desc.dtype)
+    pac = _ck_ptr(ctx, w, "a_ck", a_ck, desc.rows, _a_channels(desc))
+    ctx.check(lib().revnet_act_bwd(ctx.h, C.byref(desc), _P(pc), _P(pda), _P(pdx), _P(pac), _P(_stream_of(ctx))), w)
+
+
+def _norm_ptrs(ctx, w, d, stream, branch, channels, ck):
+    out = {n: _row_ptr(ctx, w, n, t, d.rows, d.channels, d.ld_stream, d.stream_dtype) for n, t in stream}
+    out.update((n, _row_ptr(ctx, w, n, t, d.rows, d.channels, d.ld_branch, d.branch_dtype)) for n, t in branch)
+    out.update((n, _flat_ptr(ctx, w, n, t, d.rows if n == "rstd" else d.channels)) for n, t in channels)
+    out["ck"] = _ck_ptr(ctx, w, "ck", ck, d.rows, d.channels)
+    return {n: _P(p) for n, p in out.items()}
+
+
+def revnet_rmsnorm_fwd(ctx, desc, x, r, gamma, h, n, ck, rstd):
+    w = "revnet_rmsnorm_fwd"
+    p = _norm_ptrs(ctx, w, desc, (("x", x), ("h", h)), (("r", r), ("n", n)), (("gamma", gamma), ("rstd", rstd)), ck)
+    ctx.check(lib().revnet_rmsnorm_fwd(ctx.h, C.byref(desc), p["x"], p["r"], p["gamma"], p["h"], p["n"], p["ck"], p["rstd"], _P(_stream_of(ctx))), w)
+
+
+def revnet_rmsnorm_workspace_bytes(ctx, desc) -> int:
+    n = C.c_size_t()
+    ctx.check(lib().revnet_rmsnorm_workspace_bytes(ctx.h, C.byref(desc), C.byref(n)), "revnet_rmsnorm_workspace_bytes")
+    return n.value
+
+
+def revnet_rmsnorm_bwd(ctx, desc, dn, dh, h, ck, rstd, gamma, dx, dr, dgamma, workspace):
+    w = "revnet_rmsnorm_bwd"
+    p = _norm_ptrs(ctx, w, desc, (("dh", dh), ("h", h), ("dx", dx)), (("dn", dn), ("dr", dr)), (("rstd", rstd), ("gamma", gamma), ("dgamma", dgamma)), ck)
+    size = C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size())
+    ctx.check(lib().revnet_rmsnorm_bwd(ctx.h, C.byref(desc), p["dn"], p["dh"], p["h"], p["ck"], p["rstd"], p["gamma"], p["dx"], p["dr"], p["dgamma"],
+                                       _ptr(workspace), size, _P(_stream_of(ctx))), w)
+
+
+def revnet_linear_wgrad_workspace_bytes(ctx, desc) -> int:
+    n = C.c_size_t()
+    ctx.check(lib().revnet_linear_wgrad_workspace_bytes(ctx.h, C.byref(desc), C.byref(n)), "revnet_linear_wgrad_workspace_bytes")
+    return n.value
+
+
+def revnet_linear_wgrad(ctx, desc, dy, ck, gamma, dW, workspace):
+    w = "revnet_linear_wgrad"
+    pdy = _row_ptr(ctx, w, "dy", dy, desc.rows, desc.cout, desc.ld_dy, desc.dy_dtype)
+    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.cin)
+    pg = _flat_ptr(ctx, w, "gamma", gamma, desc.cin)
+    pw = _flat_ptr(ctx, w, "dW", dW, desc.cin * desc.cout)
+    size = C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size())
+    ctx.check(lib().revnet_linear_wgrad(ctx.h, C.byref(desc), _P(pdy), _P(pc), _P(pg), _P(pw), _ptr(workspace), size, _P(_stream_of(ctx))), w)
+
+
+def revnet_logprobs_fwd(ctx, desc, logits, targets, logp, entropy, lse, top_logp=None, top_index=None):
+    w = "revnet_logprobs_fwd"
+    px = _row_ptr(ctx, w, "logits", logits, desc.rows, desc.vocab, desc.ld, desc.dtype)
+    pt = _flat_ptr(ctx, w, "targets", targets, desc.rows, "torch.int32")
+    rows = [_P(_flat_ptr(ctx, w, n, t, desc.rows)) for n, t in (("logp", logp), ("entropy", entropy), ("lse", lse))]
+    pl = _flat_ptr(ctx, w, "top_logp", top_logp, desc.rows * desc.k)
+    pi = _flat_ptr(ctx, w, "top_index", top_index, desc.rows * desc.k, "torch.int32")
+    ctx.check(lib().revnet_logprobs_fwd(ctx.h, C.byref(desc), _P(px), _P(pt), *rows, _P(pl), _P(pi), _P(_stream_of(ctx))), w)
+
+
+def revnet_logprobs_bwd(ctx, desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits):
+    w = "revnet_logprobs_bwd"
+    px = _row_ptr(ctx, w, "logits", logits, desc.rows, desc.vocab, desc.ld, desc.dtype)
+    pd = _row_ptr(ctx, w, "dlogits", dlogits, desc.rows, desc.vocab, desc.ld, desc.dtype)
+    pt = _flat_ptr(ctx, w, "targets", targets, desc.rows, "torch.int32")
+    rows = [_P(_flat_ptr(ctx, w, n, t, desc.rows)) for n, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy))]
+    ctx.check(lib().revnet_logprobs_bwd(ctx.h, C.byref(desc), _P(px), _P(pt), *rows, _P(pd), _P(_stream_of(ctx))), w)

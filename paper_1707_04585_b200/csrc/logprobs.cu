@@ -1,0 +1,324 @@
+// Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits, and the gradient.
+//
+//   forward   m = max x, s = sum e^(x - m), t = sum (x - m) e^(x - m):  lse = m + log s, entropy = log s - t / s
+//   backward  dx = dlogp (1[target] - p) - dentropy p (log p + entropy),  p = e^(x - lse)
+//
+// HBM bounds both: the logits are read once.  A thread carries the running (m, s, t) of its elements and rescales them when its maximum
+// rises; the threads' triples are joined at the end by the same rule.  With few rows a row is split over the CTAs of a cluster, which
+// join through distributed shared memory: no workspace, no second launch.
+// The k most likely tokens: every warp keeps a sorted list of its own, one entry per lane, of keys (logit, then the lower index) as 64-bit
+// integers.  A vector of logits is looked at again only if one of them reaches the list's last entry, which after the first few hundred
+// is rare in any order but an ascending one (n elements in random order change a list k ln(n / k) times).
+// Rows need not be aligned: elements in front of the first 32-byte boundary and behind the last are read one by one.
+#include "token.cuh"
+#include <math.h>
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct LogpArgs {
+    const void *x;
+    const int32_t *targets;
+    const float *lse_in, *ent_in, *dlogp, *dent;
+    float *logp, *ent, *lse, *top_logp;
+    int32_t *top_index;
+    void *dx;
+    int64_t rows, ld;
+    int vocab, k, chunk;             // chunk: logits per CTA of a cluster (forward), per CTA (backward)
+    FastDiv chunks;                  // CTAs per row (backward)
+    int *status;
+};
+
+// a row's running sums: m the maximum (in units of log 2: y = x log2 e), s = sum 2^(y - m), t = sum (y - m) 2^(y - m)
+struct Sums { float m, s, t; };
+__device__ __forceinline__ float exp2_fast(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+// a's sums as they are for the maximum m >= a.m; an empty or all -inf one (m = -inf) is zero for any m
+__device__ __forceinline__ void rescale(Sums &a, float m) {
+    if (a.m == -INFINITY || a.m == m) { a.m = m; return; }
+    const float d = a.m - m, e = exp2_fast(d);
+    a.t = (a.t + d * a.s) * e;
+    a.s *= e;
+    if (e == 0.f) a.t = 0.f;         // d = -inf: m is +inf, and the row's sums are NaN through its own element
+    a.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+    const float m = fmaxf(a.m, b.m);
+    rescale(a, m);
+    rescale(b, m);
+    return Sums{m, a.s + b.s, a.t + b.t};
+}
+// N logits
+template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N]) {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < N; i++) top = fmaxf(top, x[i]);
+    top *= kLog2e;
+    if (top > a.m) rescale(a, top);
+    // (a.m stays -inf while every logit so far is: then all differences would be NaN)
+    const float m = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float d = fmaf(x[i], kLog2e, -m), e = exp2_fast(d);
+        a.s += e;
+        a.t = fmaf(fmaxf(d, -200.f), e, a.t);        // 0 log 0 = 0: e is 0 far before -200 (fmaxf also drops a NaN, which s carries)
+    }
+}
+
+// ---- most likely tokens
+__device__ __forceinline__ unsigned long long key_of(float x, int index) {
+    x += 0.f;                                        // -0 -> 0: equal logits are equal keys
+    uint32_t b = __float_as_uint(x);
+    b = x != x ? 0xffffffffu : (b & 0x80000000u ? ~b : b | 0x80000000u);
+    return (unsigned long long)b << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ float value_of(unsigned long long key) {
+    const uint32_t b = (uint32_t)(key >> 32);
+    return b == 0xffffffffu ? NAN : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
+struct TopList {                     // lane i: the i-th largest key so far, 0 for none; last: the k-th
+    unsigned long long mine, last;
+    int k;
+    __device__ __forceinline__ void offer(unsigned long long key) {       // one key per lane; the whole warp calls
+        unsigned todo = __ballot_sync(0xffffffffu, key > last);
+        const int lane = threadIdx.x & 31;
+        while (todo) {
+            const int src = __ffs(todo) - 1;
+            todo &= todo - 1;
+            const unsigned long long c = __shfl_sync(0xffffffffu, key, src);
+            if (c <= last) continue;
+            const int at = __popc(__ballot_sync(0xffffffffu, mine > c));
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, mine, 1);
+            mine = lane < at ? mine : (lane == at ? c : up);
+            last = __shfl_sync(0xffffffffu, mine, k - 1);
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// the same shared-memory location in CTA `rank` of the cluster
+template <class T> __device__ __forceinline__ T remote(const T *p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    T v;
+    if constexpr (sizeof(T) == 8) { unsigned long long u; asm volatile("ld.shared::cluster.b64 %0, [%1];" : "=l"(u) : "r"(a) : "memory"); v = (T)u; }
+    else { uint32_t u; asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(u) : "r"(a) : "memory"); v = __uint_as_float(u); }
+    return v;
+}
+
+// not above 0, which rounding could otherwise reach
+__device__ __forceinline__ float log_prob(float x, double lse, bool none) {
+    const float v = (float)((double)x - lse);
+    return none ? -INFINITY : (v > 0.f ? 0.f : v);
+}
+
+constexpr int kVec = 16;             // logits per step of a thread
+
+// CLUSTER: the row's CTAs are a cluster along x; else one CTA per row
+template <class T, bool TOP, bool CLUSTER>
+__global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
+    __shared__ float sm_m[16], sm_s[16], sm_t[16];
+    __shared__ unsigned long long lists[TOP ? 16 * 32 : 1];
+    pdl_enter();
+    const uint32_t rank = CLUSTER ? cluster_rank() : 0, ctas = CLUSTER ? cluster_size() : 1;
+    const size_t row = blockIdx.x / ctas;
+    const T *x = (const T *)p.x + row * p.ld;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int begin = (int)rank * p.chunk, end = min(p.vocab, begin + p.chunk);
+    const int len = end > begin ? end - begin : 0;
+    // head: up to the first 32-byte boundary; body: vectors; tail
+    const T *xb = x + begin;
+    const int head = min(len, (int)((32 - ((uintptr_t)xb & 31)) & 31) / (int)sizeof(T));
+    const int vecs = (len - head) / kVec, tail0 = head + vecs * kVec;
+    Sums sum{-INFINITY, 0.f, 0.f};
+    TopList list{0ull, 0ull, p.k};
+
+    // whole warps go round the loop: the list's shuffles need all lanes
+    for (int v0 = warp * 32; v0 < vecs; v0 += blockDim.x) {
+        const int v = v0 + lane;
+        const bool ok = v < vecs;
+        float f[kVec];
+        if (ok) load16(xb + head + v * kVec, kVec, 2, f);
+        else {
+#pragma unroll
+            for (int i = 0; i < kVec; i++) f[i] = -INFINITY;
+        }
+        if (ok) add(sum, f);
+        if constexpr (TOP) {
+            float top = f[0];
+            bool odd = f[0] != f[0];
+#pragma unroll
+            for (int i = 1; i < kVec; i++) { top = fmaxf(top, f[i]); odd |= f[i] != f[i]; }
+            const bool look = ok && (odd || key_of(top, 0) >= (list.last & 0xffffffff00000000ull));
+            if (__ballot_sync(0xffffffffu, look)) {
+#pragma unroll
+                for (int i = 0; i < kVec; i++) list.offer(look ? key_of(f[i], begin + head + v * kVec + i) : 0ull);
+            }
+        }
+    }
+    for (int e0 = warp * 32; e0 < head + len - tail0; e0 += blockDim.x) {
+        const int e = e0 + lane;
+        const bool ok = e < head + len - tail0;
+        const int i = e < head ? e : tail0 + e - head;
+        const float f[1] = {ok ? to_f(xb[i]) : -INFINITY};
+        if (ok) add(sum, f);
+        if constexpr (TOP) list.offer(ok ? key_of(f[0], begin + i) : 0ull);
+    }
+    for (int o = 16; o; o >>= 1) {
+        const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
+        sum = join(sum, b);
+    }
+    if (lane == 0) { sm_m[warp] = sum.m; sm_s[warp] = sum.s; sm_t[warp] = sum.t; }
+    if constexpr (TOP) lists[warp * 32 + lane] = list.mine;
+    __syncthreads();
+    if (warp == 0) {
+        // lane w: the sums of warp w
+        sum = lane < warps ? Sums{sm_m[lane], sm_s[lane], sm_t[lane]} : Sums{-INFINITY, 0.f, 0.f};
+        for (int o = 16; o; o >>= 1) {
+            const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
+            sum = join(sum, b);
+        }
+        if constexpr (TOP) {
+            for (int w = 1; w < warps; w++) list.offer(lane < p.k ? lists[w * 32 + lane] : 0ull);
+            if (CLUSTER) { __syncwarp(); lists[lane] = list.mine; }
+        }
+        if (CLUSTER && lane == 0) { sm_m[0] = sum.m; sm_s[0] = sum.s; sm_t[0] = sum.t; }
+    }
+    if (CLUSTER) {
+        cluster_sync();
+        if (rank == 0 && warp == 0) {
+            sum = lane < (int)ctas ? Sums{remote(&sm_m[0], lane), remote(&sm_s[0], lane), remote(&sm_t[0], lane)} : Sums{-INFINITY, 0.f, 0.f};
+            for (int o = 16; o; o >>= 1) {
+                const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
+                sum = join(sum, b);
+            }
+            if constexpr (TOP)
+                for (uint32_t c = 1; c < ctas; c++) list.offer(lane < p.k ? remote(&lists[lane], c) : 0ull);
+        }
+        cluster_sync();              // nobody leaves while rank 0 reads
+        if (rank != 0) return;
+    }
+    if (warp != 0) return;
+    // once per row, in double: y = x kLog2e with the float kLog2e, so m / kLog2e is the largest logit without the rounding of m, which s makes up for
+    const bool none = sum.m == -INFINITY && sum.s == 0.f;
+    const double logs = (double)logf(sum.s), lse = none ? (double)-INFINITY : (double)sum.m / (double)kLog2e + logs;
+    if (lane == 0) {
+        if (p.lse) p.lse[row] = (float)lse;
+        if (p.ent) { const float h = (float)(logs - (double)kLn2 * ((double)sum.t / sum.s)); p.ent[row] = none || h < 0.f ? 0.f : h; }
+        if (p.logp) {
+            const int tgt = p.targets[row];
+            float v = 0.f;
+            if (tgt >= 0 && tgt < p.vocab) v = log_prob(to_f(x[tgt]), lse, none);
+            else if (tgt != -1) { v = NAN; atomicExch(p.status, (int)REVNET_E_INVALID_ARG); }
+            p.logp[row] = v;
+        }
+    }
+    if constexpr (TOP)
+        if (lane < p.k) {
+            p.top_index[row * p.k + lane] = (int)~(uint32_t)list.mine;
+            p.top_logp[row * p.k + lane] = log_prob(value_of(list.mine), lse, none);
+        }
+}
+
+// one logit's gradient
+__device__ __forceinline__ float grad(float x, float lse, float g, float ge, float ent2) {
+    const float l = (x - lse) * kLog2e, q = exp2_fast(l);
+    // ge log p in natural units: ge (l + ent2) ln 2, the factor folded into ge by the caller
+    return q == 0.f ? 0.f : -q * fmaf(ge, l + ent2, g);
+}
+template <class T>
+__global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogpArgs p) {
+    pdl_enter();
+    uint32_t r, c;
+    p.chunks.divmod(blockIdx.x, r, c);
+    const size_t row = r;
+    const T *x = (const T *)p.x + row * p.ld + (size_t)c * p.chunk;
+    T *dx = (T *)p.dx + row * p.ld + (size_t)c * p.chunk;
+    const int begin = (int)c * p.chunk, len = min(p.chunk, p.vocab - begin);
+    const float lse = p.lse_in[row];
+    int tgt = -1;
+    float g = 0.f, ge = 0.f, ent2 = 0.f;
+    if (p.dlogp) {
+        tgt = p.targets[row];
+        if (tgt != -1) g = p.dlogp[row];
+        if (tgt < -1 || tgt >= p.vocab) {
+            g = NAN;
+            if (threadIdx.x == 0) atomicExch(p.status, (int)REVNET_E_INVALID_ARG);
+        }
+    }
+    if (p.dent) { ge = p.dent[row] * kLn2; ent2 = p.ent_in[row] * kLog2e; }
+    const bool none = lse == -INFINITY;
+    // vectors where both rows have their 32-byte boundaries at the same elements
+    const bool same = (((uintptr_t)x ^ (uintptr_t)dx) & 31) == 0;
+    const int head = same ? min(len, (int)((32 - ((uintptr_t)x & 31)) & 31) / (int)sizeof(T)) : len;
+    const int vecs = (len - head) / kVec, tail0 = head + vecs * kVec;
+    for (int v = threadIdx.x; v < vecs; v += blockDim.x) {
+        float f[kVec];
+        load16(x + head + v * kVec, kVec, 2, f);
+        const int at = tgt - (begin + head + v * kVec);
+#pragma unroll
+        for (int i = 0; i < kVec; i++) {
+            const float d = none ? 0.f : grad(f[i], lse, g, ge, ent2);
+            f[i] = at == i && !none ? d + g : d;
+        }
+        store16(dx + head + v * kVec, kVec, 2, f);
+    }
+    for (int e = threadIdx.x; e < head + len - tail0; e += blockDim.x) {
+        const int i = e < head ? e : tail0 + e - head;
+        float d = none ? 0.f : grad(to_f(x[i]), lse, g, ge, ent2);
+        if (begin + i == tgt && !none) d += g;
+        put(dx[i], d);
+    }
+}
+
+template <class T> void fwd_t(Exec &ex, const LogpArgs &p, int cluster, unsigned threads) {
+    const unsigned rows = (unsigned)p.rows;
+    if (cluster == 1) {
+        if (p.k) launch(ex, logprobs_fwd_kernel<T, true, false>, rows, threads, 0, p);
+        else launch(ex, logprobs_fwd_kernel<T, false, false>, rows, threads, 0, p);
+    } else {
+        if (p.k) launch_cluster(ex, logprobs_fwd_kernel<T, true, true>, rows * cluster, threads, 0, cluster, p);
+        else launch_cluster(ex, logprobs_fwd_kernel<T, false, true>, rows * cluster, threads, 0, cluster, p);
+    }
+}
+
+}  // namespace
+
+void logprobs_fwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, const int32_t *targets, float *logp, float *entropy, float *lse,
+                  float *top_logp, int32_t *top_index) {
+    if (d.rows == 0) return;
+    LogpArgs p{};
+    p.x = logits; p.targets = targets; p.logp = logp; p.ent = entropy; p.lse = lse; p.top_logp = top_logp; p.top_index = top_index;
+    p.rows = d.rows; p.ld = d.ld; p.vocab = d.vocab; p.k = d.k; p.status = ex.ctx->dev_status;
+    unsigned threads = 32;
+    while (threads < 512 && (int)threads * kVec < d.vocab) threads *= 2;
+    // a row is split while its parts stay longer than one step of a CTA and the GPU has SMs to spare
+    int cluster = 1;
+    while (cluster < 8 && d.rows * cluster * 2 <= 2 * ex.ctx->sm_count && d.vocab / (cluster * 2) >= (int)threads * kVec) cluster *= 2;
+    p.chunk = (d.vocab + cluster - 1) / cluster;
+    const double bytes = (double)d.rows * d.vocab * (d.dtype == REVNET_F32 ? 4 : 2);
+    if (d.dtype == REVNET_F32) fwd_t<float>(ex, p, cluster, threads);
+    else fwd_t<bf16>(ex, p, cluster, threads);
+    ex.check("logprobs_fwd", bytes);
+}
+
+void logprobs_bwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, const int32_t *targets, const float *lse, const float *entropy,
+                  const float *dlogp, const float *dentropy, void *dlogits) {
+    if (d.rows == 0) return;
+    LogpArgs p{};
+    p.x = logits; p.targets = targets; p.lse_in = lse; p.ent_in = entropy; p.dlogp = dlogp; p.dent = dentropy; p.dx = dlogits;
+    p.rows = d.rows; p.ld = d.ld; p.vocab = d.vocab; p.status = ex.ctx->dev_status;
+    unsigned threads = 32;
+    while (threads < 256 && (int)threads * kVec < d.vocab) threads *= 2;
+    p.chunk = (int)threads * kVec * 2;
+    int64_t chunks = (d.vocab + p.chunk - 1) / p.chunk;
+    while (chunks > 1 && d.rows * chunks >= (int64_t(1) << 31)) { p.chunk *= 2; chunks = (d.vocab + p.chunk - 1) / p.chunk; }
+    p.chunks = fast_div((uint32_t)chunks);
+    const double bytes = (double)d.rows * d.vocab * (d.dtype == REVNET_F32 ? 8 : 4);
+    const unsigned grid = (unsigned)(d.rows * chunks);
+    if (d.dtype == REVNET_F32) launch_stream(ex, bytes, 0, logprobs_bwd_kernel<float>, grid, threads, 0, p);
+    else launch_stream(ex, bytes, 0, logprobs_bwd_kernel<bf16>, grid, threads, 0, p);
+    ex.check("logprobs_bwd", bytes);
+}

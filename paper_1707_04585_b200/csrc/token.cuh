@@ -1,0 +1,226 @@
+// Shared by the operators on rows of tokens: loads and stores of sixteen channels, and the 8-bit checkpoint format
+// (include/revnet.h, "An 8-bit checkpoint").
+#pragma once
+#include "common.cuh"
+#include <cuda_fp8.h>
+
+// A thread's unit of work in the elementwise kernels is a group of 16 consecutive channels: 16 code bytes are one 16-byte access, 16 bf16
+// one of 32 bytes, and the two lanes 2i, 2i + 1 hold the 32 channels that share a scale.
+constexpr int kGroup = 16;
+
+// ---------------------------------------------------------------- host side
+struct Checkpoint {            // a checkpoint buffer taken apart
+    uint8_t *codes, *scales;
+    int pitch;                 // bytes per row of codes: channels rounded up to 32
+    uint32_t rows_pad;         // rows rounded up to 64
+};
+static inline int ck_pitch(int channels) { return (channels + 31) & ~31; }
+static inline size_t ck_scales_at(int64_t rows, int channels) { return ((size_t)rows * ck_pitch(channels) + 255) & ~size_t(255); }
+static inline size_t ck_bytes(int64_t rows, int channels) {
+    return ck_scales_at(rows, channels) + (size_t)((channels + 127) / 128) * (((size_t)rows + 63) & ~size_t(63)) * 4;
+}
+static inline Checkpoint ck_view(const void *buf, int64_t rows, int channels) {
+    uint8_t *b = (uint8_t *)buf;
+    return Checkpoint{b, b ? b + ck_scales_at(rows, channels) : nullptr, ck_pitch(channels), (uint32_t)((rows + 63) & ~int64_t(63))};
+}
+// How wide a thread may access the rows of a tensor at p, `ld` elements of `size` bytes apart, at multiples of 16 channels:
+// 2: 32 bytes, 1: 16 bytes, 0: element by element.
+static inline int access_level(const void *p, int64_t ld, int size) {
+    const uint64_t a = (uint64_t)(uintptr_t)p | (uint64_t)ld * size;
+    return a % 32 == 0 ? 2 : (a % 16 == 0 ? 1 : 0);
+}
+
+// ---------------------------------------------------------------- act8.cu, norm.cu, wgrad8.cu, logprobs.cu
+void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a);
+void act8_load(Exec &ex, const revnet_act_desc &d, const void *ck, void *a);
+void act8_bwd(Exec &ex, const revnet_act_desc &d, const void *ck, const void *da, void *dx, void *a_ck);
+void rmsnorm_fwd(Exec &ex, const revnet_norm_desc &d, const void *x, const void *r, const float *gamma, void *h, void *n, void *ck, float *rstd);
+size_t rmsnorm_bwd_workspace(const revnet_ctx *ctx, const revnet_norm_desc &d);
+void rmsnorm_bwd(Exec &ex, const revnet_norm_desc &d, const void *dn, const void *dh, const void *h, const void *ck, const float *rstd,
+                 const float *gamma, void *dx, void *dr, float *dgamma, float *partial);
+size_t wgrad8_workspace(const revnet_ctx *ctx, const revnet_wgrad_desc &d);
+void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck, const float *gamma, float *dW, char *workspace);
+void logprobs_fwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, const int32_t *targets, float *logp, float *entropy, float *lse,
+                  float *top_logp, int32_t *top_index);
+void logprobs_bwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, const int32_t *targets, const float *lse, const float *entropy,
+                  const float *dlogp, const float *dentropy, void *dlogits);
+
+#ifdef __CUDACC__
+// ---------------------------------------------------------------- sixteen channels of a row
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void put(float &d, float v) { d = v; }
+__device__ __forceinline__ void put(bf16 &d, float v) { d = __float2bfloat16_rn(v); }
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+__device__ __forceinline__ uint32_t byte_of(const uint8_t *p) { return *p; }
+
+// raw words of 16 elements, so that a load can be in flight while earlier values are worked on
+template <class T> struct Raw16 { uint32_t w[16 * sizeof(T) / 4]; };
+
+// elements p[0 .. n), n <= 16 (n <= 0: none), zeros behind them
+template <class T> __device__ __forceinline__ void load_raw(const T *p, int n, int level, Raw16<T> &r) {
+    constexpr int W = 16 * sizeof(T) / 4;
+    if (n >= 16 && level == 2) {
+#pragma unroll
+        for (int i = 0; i < W; i += 8) {
+            uint32_t t[8];
+            ld8(reinterpret_cast<const char *>(p) + 4 * i, t, true);
+#pragma unroll
+            for (int j = 0; j < 8; j++) r.w[i + j] = t[j];
+        }
+    } else if (n >= 16 && level == 1) {
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
+            r.w[i] = q.x; r.w[i + 1] = q.y; r.w[i + 2] = q.z; r.w[i + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i++) {
+            if constexpr (sizeof(T) == 4) {
+                r.w[i] = i < n ? __float_as_uint(to_f(p[i])) : 0u;
+            } else {
+                const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
+                const uint32_t lo = 2 * i < n ? s[2 * i] : 0u, hi = 2 * i + 1 < n ? s[2 * i + 1] : 0u;
+                r.w[i] = lo | hi << 16;
+            }
+        }
+    }
+}
+__device__ __forceinline__ void unpack(const Raw16<float> &r, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r.w[i]);
+}
+__device__ __forceinline__ void unpack(const Raw16<bf16> &r, float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) { v[2 * i] = bf16_lo(r.w[i]); v[2 * i + 1] = bf16_hi(r.w[i]); }
+}
+__device__ __forceinline__ void pack(const float (&v)[16], Raw16<float> &r) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) r.w[i] = __float_as_uint(v[i]);
+}
+// bf16 outputs: the one rounding of a value, to nearest even
+__device__ __forceinline__ void pack(const float (&v)[16], Raw16<bf16> &r) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) r.w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+}
+template <class T> __device__ __forceinline__ void store_raw(T *p, int n, int level, const Raw16<T> &r) {
+    constexpr int W = 16 * sizeof(T) / 4;
+    if (n >= 16 && level == 2) {
+#pragma unroll
+        for (int i = 0; i < W; i += 8) {
+            uint32_t t[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) t[j] = r.w[i + j];
+            st8(reinterpret_cast<char *>(p) + 4 * i, t, true);
+        }
+    } else if (n >= 16 && level == 1) {
+#pragma unroll
+        for (int i = 0; i < W; i += 4)
+            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p) + 4 * i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i++) {
+            if constexpr (sizeof(T) == 4) {
+                if (i < n) reinterpret_cast<uint32_t *>(p)[i] = r.w[i];
+            } else {
+                uint16_t *s = reinterpret_cast<uint16_t *>(p);
+                if (2 * i < n) s[2 * i] = (uint16_t)r.w[i];
+                if (2 * i + 1 < n) s[2 * i + 1] = (uint16_t)(r.w[i] >> 16);
+            }
+        }
+    }
+}
+template <class T> __device__ __forceinline__ void load16(const T *p, int n, int level, float (&v)[16]) {
+    Raw16<T> r;
+    load_raw(p, n, level, r);
+    unpack(r, v);
+}
+template <class T> __device__ __forceinline__ void store16(T *p, int n, int level, const float (&v)[16]) {
+    Raw16<T> r;
+    pack(v, r);
+    store_raw(p, n, level, r);
+}
+
+// ---------------------------------------------------------------- codes
+// Scale byte of a block whose largest magnitude has the bits `top` (sign cleared): the exponent field of the smallest power of two s with
+// top <= 127 s (448 s), read off the bits: 127 = 1.984375 * 2^6, 448 = 1.75 * 2^8, so it is top's exponent - 6 (- 8), one more where top's
+// mantissa exceeds that of 127 (448).  Not below 10 (2^-117), so that the least value, 2^-9 * 2^-117 in e4m3, is a normal bf16 number;
+// 255 for an infinity or a NaN, whose bits are the largest.
+template <int CODE> __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+    if (top >= 0x7f800000u) return 255u;
+    const uint32_t m = top & 0x7fffffu;
+    const int e = (int)(top >> 23) - (CODE == REVNET_INT8 ? 6 : 8) + (m > (CODE == REVNET_INT8 ? 0x7e0000u : 0x600000u) ? 1 : 0);
+    return (uint32_t)(e < 10 ? 10 : e);
+}
+__device__ __forceinline__ uint32_t abs_max16(const float (&v)[16]) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t = max(t, __float_as_uint(v[i]) & 0x7fffffffu);
+    return t;
+}
+// codes of 16 values: the multiplication by a power of two is exact, the one rounding is to nearest even
+template <int CODE> __device__ __forceinline__ uint4 encode16(const float (&v)[16], uint32_t byte) {
+    uint32_t w[4];
+    if (byte == 255u) return make_uint4(0u, 0u, 0u, 0u);
+    const float inv = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (CODE == REVNET_INT8) {
+            // 1.5 * 2^23 added: the sum's last mantissa bits are the integer nearest to v * inv, in two's complement
+            uint32_t b[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) b[j] = __float_as_uint(__fmaf_rn(v[4 * i + j], inv, 12582912.f));
+            w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+        } else {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i] * inv, v[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2] * inv, v[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+            w[i] = lo | hi << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// sign, 4 exponent and 3 mantissa bits of an e4m3 byte moved to a float's places: the exponent's bias is 7 and not 127, which the factor 2^120
+// makes up for (subnormal codes included)
+__device__ __forceinline__ float e4m3_to_f(uint32_t b) {
+    return __uint_as_float((b & 0x80u) << 24 | (b & 0x7fu) << 20) * __uint_as_float((120u + 127u) << 23);
+}
+template <int CODE> __device__ __forceinline__ void decode16(uint4 q, uint32_t byte, float (&v)[16]) {
+    const float s = __uint_as_float(byte << 23);             // byte 255: infinity, and 0 * infinity = NaN
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (CODE == REVNET_INT8) {
+            const uint32_t u = w[i] ^ 0x80808080u;           // code + 128 in each byte: 2^23 + that is a float whose last byte it is
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[4 * i + j] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + j)) - 8388736.f) * s;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[4 * i + j] = e4m3_to_f(w[i] >> (8 * j)) * s;
+        }
+    }
+}
+__device__ __forceinline__ size_t scale_index(const Checkpoint &ck, size_t row, int ch) {
+    return ((size_t)(ch >> 7) * ck.rows_pad + row) * 4 + ((ch >> 5) & 3);
+}
+// 16 channels into a checkpoint, by both lanes of a pair at once (all lanes of the warp call it; live: the group lies inside the
+// padded row); v holds zeros behind the row's last channel
+template <int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16]) {
+    uint32_t top = abs_max16(v);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t byte = scale_byte<CODE>(top);
+    if (!live) return;
+    *reinterpret_cast<uint4 *>(ck.codes + row * ck.pitch + ch) = encode16<CODE>(v, byte);
+    if ((ch & 16) == 0) ck.scales[scale_index(ck, row, ch)] = (uint8_t)byte;
+}
+// 16 channels from a checkpoint, ch a multiple of 16
+template <int CODE> __device__ __forceinline__ void read16(const Checkpoint &ck, size_t row, int ch, float (&v)[16]) {
+    const uint4 q = *reinterpret_cast<const uint4 *>(ck.codes + row * ck.pitch + ch);
+    decode16<CODE>(q, byte_of(ck.scales + scale_index(ck, row, ch)), v);
+}
+#endif
