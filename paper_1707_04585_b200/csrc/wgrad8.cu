@@ -5,35 +5,41 @@
 //
 //   dy     TMA -> shared memory, 64 rows x 64 channels per box, 128-byte swizzle, M-major: the A operand as it lies
 //   codes  TMA -> shared memory (64 rows x 128 channels) -> eight decoder warps -> bf16 in the same swizzled layout: the B operand
-//   D      512 (or 256) output channels x 256 input channels of fp32 in the pair's tensor memory
+//   D      256 output channels x 256 input channels of fp32 in the pair's tensor memory, twice
 //
-// What bounds it: shared memory and the tensor pipe about equally.  Decoding is on the side of N because an MMA of the pair reuses a
-// decoded element for all its 512 rows: per 64 rows a CTA loads 32 KB of dy and 8 KB of codes and decodes 8192 values for 1024 clocks
-// of MMAs.  (With x on the side of M it would decode twice as many, and shared memory would carry 144 bytes per clock, of 128.)
+// Long sums: the tensor cores round their running sum towards zero, an error that grows with the number of rows (7.8e-6 relative after about
+// 10000).  So a run of MMAs covers 1024 rows; the decoder warps then add its result to sums in registers (128 per thread), to nearest,
+// while the MMAs of the next run fill the other half of tensor memory.
 //
-// The products of a tile (over all rows) are one after another and the tiles are cut where the pairs' shares end: pair p of P works on
-// steps [p n / P, (p + 1) n / P) of the n = tiles x (64-row steps), so every SM is busy to the end for any shape.  A tile that one pair
-// finishes goes straight to dW; parts of a tile go to the workspace, and a second kernel adds them in a fixed order.
+// Schedule: with P pairs resident, pair p takes the tiles p, p + P, ... as long as there is one for every pair, all of them at the same rows
+// at the same time (so that L2 serves what they share); the steps of the tiles left over are dealt out evenly, tile after tile, pair p of P'
+// getting [p n / P', (p + 1) n / P').  Parts of a tile go to the workspace, and a second kernel adds them in a fixed order.
 #include "token.cuh"
 #include "tc_ptx.cuh"
 
 namespace {
 using namespace tc;
 
-constexpr int kThreads = 384;        // warp 0: dy loads, 1: MMAs, 2: codes, 3: tensor memory; 4..11: decoders, which also store the tiles
-constexpr int kDecoders = 8;
+constexpr int kThreads = 768;        // warp 0: dy loads, 1: MMAs, 2: codes, 3: tensor memory; 4..11: decoders, which also keep and store the sums
+constexpr int kSummers = 8, kDecoders = 12;
+constexpr int kGroups = 3, kGroupWarps = kDecoders / kGroups;    // every kGroups-th step is decoded by the same kGroupWarps warps
+constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
+static_assert((4 + kDecoders) * kRegsFew + kSummers * kRegsSums == kThreads / 32 * kRegs, "the split is the launch's total");
 constexpr int kStep = 64;            // rows per step
-constexpr int kN = 256;              // input channels of a pair's tile, half of them per CTA
+constexpr int kRun = 16;             // steps per run of the tensor cores' own sum
+constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
 constexpr int kStepsMin = 8;         // a pair's share is at least that long where the work allows: shorter ones do not pay for their sums
 constexpr uint32_t kBlock = 64 * 128;        // bytes of 64 rows x 64 channels of bf16, the unit of both operands
+constexpr int kA = 5, kB = 6, kC = 6;        // stages of the rings: dy, decoded x, codes
+// A group meets every phase of the barriers that it waits on only if a stage is always the same group's: else it could take the phase before the
+// one it wants, of the same parity as the one before that, for complete.
+static_assert(kB % kGroups == 0 && kC % kGroups == 0, "a stage belongs to one group");
+constexpr uint32_t kOperand = 2 * kBlock, kCodes = kStep * 128;
+constexpr uint32_t kSmem = kA * kOperand + kB * kOperand + kC * (kCodes + kStep * 4) + 1024;
+constexpr size_t kSlot = (size_t)kM * kN;    // floats of a part
 
-template <int GM> struct Tile {      // GM: groups of 128 output channels per CTA; a pair's tile has 256 GM of them
-    static constexpr int kA = GM == 2 ? 4 : 5, kB = GM == 2 ? 3 : 4, kC = GM == 2 ? 3 : 4;      // stages of the rings
-    static constexpr uint32_t kAStage = GM * 2 * kBlock, kBStage = 2 * kBlock, kCStage = kStep * 128;
-    static constexpr uint32_t kSmem = kA * kAStage + kB * kBStage + kC * (kCStage + kStep * 4) + 1024;
-};
 struct Shared {
-    uint64_t a_full[8], a_empty[8], b_full[8], b_empty[8], c_full[8], c_empty[8], d_full, d_empty;
+    uint64_t a_full[kA], a_empty[kA], b_full[kB], b_empty[kB], c_full[kC], c_empty[kC], d_full[2], d_empty[2];
     uint32_t tmem, failed;
 };
 
@@ -46,25 +52,44 @@ struct alignas(64) Wgrad8Args {
     int rows, cin, cout;
     int row_steps;                   // 64-row steps of one pass over the rows
     int steps;                       // of a tile: row_steps, or three times that (float32 dy as three bf16 parts)
-    int tiles_c, tiles;              // tiles along the input channels; in all
-    int pairs;
+    int tiles_c;                     // tiles along the input channels
+    int pairs, waves;                // every pair takes `waves` whole tiles
+    int rest, sharers;               // tiles left over, and how many pairs share their steps
     uint32_t rows_pad;
     int vec;                         // dW rows take 16-byte stores
 };
-// first step of a pair's share
-__host__ __device__ __forceinline__ int64_t share(int64_t n, int p, int pairs) { return n * p / pairs; }
-// A part of a tile: where its partial sums go.  A pair has at most two parts that are not whole tiles: the one its share starts in and the one
-// it ends in.
-__device__ __forceinline__ size_t slot_floats(int gm) { return (size_t)gm * 256 * kN; }
+// first step of pair q's share of the n steps left over (fewer than 74 tiles of fewer than 3 * 2^23 steps: below 2^31)
+__host__ __device__ __forceinline__ int share(int n, int q, int sharers) { return (int)((int64_t)n * q / sharers); }
 
-// bounded wait by one lane for its warp; false: gave up, or somebody else in the CTA did
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, uint32_t *failed, bool cluster) {
-    bool ok = true;
-    if ((threadIdx.x & 31) == 0) {
-        ok = cluster ? mbar_wait_cluster(bar, parity) : mbar_wait(bar, parity);
-        if (!ok) atomicExch(failed, 1u);
+// The pieces of work of a pair, in order; every role of both CTAs walks the same list.
+struct Pieces {
+    const Wgrad8Args &p;
+    int pair, wave = 0;
+    int from = 0, it = 0, to = 0;
+    int tile, k0, k1, slot;          // steps [k0, k1) of a tile; slot: where a part of a tile goes, -1 for a whole one
+    __device__ __forceinline__ Pieces(const Wgrad8Args &a, int q) : p(a), pair(q) {
+        const int n = a.rest * a.steps;
+        if (q < a.sharers) { from = it = share(n, q, a.sharers); to = share(n, q + 1, a.sharers); }
     }
-    return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    __device__ __forceinline__ bool next() {
+        if (wave < p.waves) { tile = pair + wave++ * p.pairs; k0 = 0; k1 = p.steps; slot = -1; return true; }
+        if (it >= to) return false;
+        const int t = it / p.steps;
+        tile = p.waves * p.pairs + t;
+        k0 = it - t * p.steps;
+        k1 = to - it < p.steps - k0 ? k0 + (to - it) : p.steps;
+        // at most two parts per pair: the tile that its share starts in, and the one that it ends in
+        slot = k0 == 0 && k1 == p.steps ? -1 : pair * 2 + (it == from ? 0 : 1);
+        it += k1 - k0;
+        return true;
+    }
+};
+
+// bounded wait of a whole warp; false: gave up
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, uint32_t *failed) {
+    const bool ok = mbar_wait(bar, parity);
+    if (!ok) atomicExch(failed, 1u);
+    return __all_sync(0xffffffffu, ok);
 }
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -75,202 +100,216 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// four codes -> four bf16, times a scale (twice the same bf16): exact
-template <int CODE> __device__ __forceinline__ uint2 decode4(uint32_t w, uint32_t scale2) {
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// two codes (the bytes that SEL puts under a bf16 exponent of 128) -> two bf16, times a scale (twice the same bf16): exact
+template <int CODE> __device__ __forceinline__ uint32_t decode2(uint32_t w, uint32_t sel, uint32_t scale2) {
     if constexpr (CODE == REVNET_INT8) {
-        const uint32_t u = w ^ 0x80808080u;
-        float f[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) f[j] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + j)) - 8388736.f;
-        return make_uint2(mul_bf16x2(bf16_pair(f[0], f[1]), scale2), mul_bf16x2(bf16_pair(f[2], f[3]), scale2));
+        // 0x43 above the byte: a bf16 in [128, 256) whose last 7 bits are the code's; the sign bit alone makes it 256 = 128 + 128
+        const uint32_t x = __byte_perm(w, 0x43434343u, sel);
+        return mul_bf16x2(sub_bf16x2(x & 0xff7fff7fu, x & 0xff80ff80u), scale2);
     } else {
-        // sign, exponent and mantissa bits in a bf16's places; its exponent bias is larger by 120
+        // sign, exponent and mantissa bits moved to a bf16's places; its exponent bias is larger by 120
         const uint32_t big = (120u + 127u) << 7 | (120u + 127u) << 23;
-        const uint32_t lo = __byte_perm(w, 0u, 0x1404), hi = __byte_perm(w, 0u, 0x3424);        // codes in the upper bytes
-        const uint32_t l = (lo & 0x80008000u) | ((lo >> 4) & 0x07f007f0u), h = (hi & 0x80008000u) | ((hi >> 4) & 0x07f007f0u);
-        return make_uint2(mul_bf16x2(mul_bf16x2(l, big), scale2), mul_bf16x2(mul_bf16x2(h, big), scale2));
+        const uint32_t x = __byte_perm(w, 0u, sel) << 8;                 // the codes in the upper bytes
+        return mul_bf16x2(mul_bf16x2((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), big), scale2);
     }
 }
 
-template <int GM, int CODE>
+template <int CODE>
 __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_constant__ Wgrad8Args p) {
-    using T = Tile<GM>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Shared sh;
     uint8_t *ring_a = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *ring_b = ring_a + T::kA * T::kAStage, *ring_c = ring_b + T::kB * T::kBStage;
-    uint32_t *ring_s = (uint32_t *)(ring_c + T::kC * T::kCStage);
+    uint8_t *ring_b = ring_a + kA * kOperand, *ring_c = ring_b + kB * kOperand;
+    uint32_t *ring_s = (uint32_t *)(ring_c + kC * kCodes);
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
-    const int pair = (int)(blockIdx.x >> 1);
-    constexpr uint32_t kCols = GM * kN;
+    Pieces job(p, (int)(blockIdx.x >> 1));
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 8; i++) {
-            mbar_init(&sh.a_full[i], 1); mbar_init(&sh.a_empty[i], 1);
-            mbar_init(&sh.b_full[i], 2 * kDecoders); mbar_init(&sh.b_empty[i], 1);
-            mbar_init(&sh.c_full[i], 1); mbar_init(&sh.c_empty[i], kDecoders);
-        }
-        mbar_init(&sh.d_full, 1); mbar_init(&sh.d_empty, 2 * kDecoders);
+        for (int i = 0; i < kA; i++) { mbar_init(&sh.a_full[i], 1); mbar_init(&sh.a_empty[i], 1); }
+        for (int i = 0; i < kB; i++) { mbar_init(&sh.b_full[i], 2 * kGroupWarps); mbar_init(&sh.b_empty[i], 1); }
+        for (int i = 0; i < kC; i++) { mbar_init(&sh.c_full[i], 1); mbar_init(&sh.c_empty[i], kGroupWarps); }
+        for (int i = 0; i < 2; i++) { mbar_init(&sh.d_full[i], 1); mbar_init(&sh.d_empty[i], 2 * kSummers); }
         sh.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 3) tmem2_alloc(&sh.tmem, kCols);
+    if (warp == 3) tmem2_alloc(&sh.tmem, 2 * kN);
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
     tc_fence_after();
     pdl_enter();
     const uint32_t tmem = sh.tmem;
-    const int64_t n = (int64_t)p.tiles * p.steps, from = share(n, pair, p.pairs), to = share(n, pair + 1, p.pairs);
 
-    // every role walks the same list of (tile, steps k0 .. k1)
-    if (warp == 0) {
+    if (warp < 4) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+      if (warp == 0) {
         const uint32_t full0 = mapa_shared(smem_u32(&sh.a_full[0]), 0);
         int s = 0; uint32_t round = 0;
         bool ok = true;
-        for (int64_t it = from; it < to && ok; it++) {
-            const int tile = (int)(it / p.steps), k = (int)(it - (int64_t)tile * p.steps);
-            const int o0 = (tile / p.tiles_c) * 256 * GM + (int)rank * 128;
-            if (round > 0) ok = warp_wait(&sh.a_empty[s], (round - 1) & 1, &sh.failed, true);
-            if (!ok) break;
-            if (elect_one()) {
-                if (rank == 0) mbar_expect_tx(&sh.a_full[s], 2 * T::kAStage);        // the leader's barrier counts the bytes of both CTAs
-#pragma unroll
-                for (int g = 0; g < GM; g++)
-#pragma unroll
-                    for (int b = 0; b < 2; b++)
-                        tma2_load_2d(ring_a + s * T::kAStage + (g * 2 + b) * kBlock, &p.dy, full0 + 8u * s, o0 + g * 256 + b * 64, k * kStep);
+        while (ok && job.next()) {
+            const int o0 = (job.tile / p.tiles_c) * kM + (int)rank * 128;
+            for (int k = job.k0; k < job.k1; k++) {
+                if (round > 0 && !(ok = warp_wait(&sh.a_empty[s], (round - 1) & 1, &sh.failed))) break;
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect_tx(&sh.a_full[s], 2 * kOperand);      // the leader's barrier counts the bytes of both CTAs
+                    tma2_load_2d(ring_a + s * kOperand, &p.dy, full0 + 8u * s, o0, k * kStep);
+                    tma2_load_2d(ring_a + s * kOperand + kBlock, &p.dy, full0 + 8u * s, o0 + 64, k * kStep);
+                }
+                __syncwarp();
+                if (++s == kA) { s = 0; round++; }
             }
-            __syncwarp();
-            if (++s == T::kA) { s = 0; round++; }
         }
-    } else if (warp == 1) {
+      } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             const uint32_t idesc = instr_desc_m256(kN) | (3u << 15);     // both operands M / N-major
             const uint64_t da0 = smem_desc_mn(smem_u32(ring_a), 128, kBlock), db0 = smem_desc_mn(smem_u32(ring_b), 128, kBlock);
-            int sa = 0, sb = 0; uint32_t ra = 0, rb = 0, tiles_done = 0;
+            int sa = 0, sb = 0; uint32_t ra = 0, rb = 0, run = 0;
             bool ok = true;
-            for (int64_t it = from; it < to && ok;) {
-                const int tile = (int)(it / p.steps);
-                const int64_t tile_end = (int64_t)(tile + 1) * p.steps, end = tile_end < to ? tile_end : to;
-                if (tiles_done > 0) ok = mbar_wait_cluster(&sh.d_empty, (tiles_done - 1) & 1);
-                tc_fence_after();
-                for (bool first = true; it < end && ok; it++) {
-                    ok = mbar_wait_cluster(&sh.a_full[sa], ra & 1) && mbar_wait_cluster(&sh.b_full[sb], rb & 1);
-                    if (!ok) break;
+            while (ok && job.next()) {
+                for (int k = job.k0; k < job.k1 && ok; run++) {
+                    const int end = k + kRun < job.k1 ? k + kRun : job.k1;
+                    if (run > 1) ok = mbar_wait(&sh.d_empty[run & 1], ((run >> 1) - 1) & 1);
                     tc_fence_after();
-                    uint64_t db = db0 + (uint32_t)sb * (T::kBStage >> 4);
-#pragma unroll
-                    for (int g = 0; g < GM; g++) {
-                        uint64_t da = da0 + (uint32_t)sa * (T::kAStage >> 4) + (uint32_t)g * (2 * kBlock >> 4);
+                    const uint32_t acc = tmem + (run & 1) * kN;
+                    for (bool first = true; k < end && ok; k++) {
+                        ok = mbar_wait(&sh.a_full[sa], ra & 1) && mbar_wait(&sh.b_full[sb], rb & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t da = da0 + (uint32_t)sa * (kOperand >> 4), db = db0 + (uint32_t)sb * (kOperand >> 4);
 #pragma unroll
                         for (int ks = 0; ks < kStep / 16; ks++)          // 16 rows of 128 bytes per MMA
-                            mma2_bf16(tmem + (uint32_t)(g * kN), da + (uint32_t)ks * 128u, db + (uint32_t)ks * 128u, idesc, first && ks == 0 ? 0u : 1u);
+                            mma2_bf16(acc, da + (uint32_t)ks * 128u, db + (uint32_t)ks * 128u, idesc, first && ks == 0 ? 0u : 1u);
+                        first = false;
+                        mma2_commit_both(&sh.a_empty[sa]);
+                        mma2_commit_both(&sh.b_empty[sb]);
+                        if (++sa == kA) { sa = 0; ra++; }
+                        if (++sb == kB) { sb = 0; rb++; }
                     }
-                    first = false;
-                    mma2_commit_both(&sh.a_empty[sa]);
-                    mma2_commit_both(&sh.b_empty[sb]);
-                    if (++sa == T::kA) { sa = 0; ra++; }
-                    if (++sb == T::kB) { sb = 0; rb++; }
+                    mma2_commit_both(&sh.d_full[run & 1]);
                 }
-                mma2_commit_both(&sh.d_full);
-                tiles_done++;
             }
             if (!ok) atomicExch(&sh.failed, 1u);
         }
-    } else if (warp == 2) {
+      } else if (warp == 2) {
         int s = 0; uint32_t round = 0;
         bool ok = true;
-        for (int64_t it = from; it < to && ok; it++) {
-            const int tile = (int)(it / p.steps), t0 = (int)((it - (int64_t)tile * p.steps) % p.row_steps) * kStep;
-            const int c0 = (tile % p.tiles_c) * kN + (int)rank * 128;
-            if (round > 0) ok = warp_wait(&sh.c_empty[s], (round - 1) & 1, &sh.failed, false);
-            if (!ok) break;
-            if (elect_one()) {
-                const bool in = c0 < p.cin;          // a CTA whose half of the tile lies behind the last channel has no scales to read
-                mbar_expect_tx(&sh.c_full[s], T::kCStage + (in ? kStep * 4 : 0));
-                tma_load_2d(ring_c + s * T::kCStage, &p.codes, &sh.c_full[s], c0, t0);
-                if (in) bulk_load(ring_s + s * kStep, p.scales + ((size_t)(c0 >> 7) * p.rows_pad + t0) * 4, kStep * 4, &sh.c_full[s]);
+        while (ok && job.next()) {
+            const int c0 = (job.tile % p.tiles_c) * kN + (int)rank * 128;
+            const bool in = c0 < p.cin;              // a CTA whose half of the tile lies behind the last channel has no scales to read
+            int t = job.k0 % p.row_steps;
+            for (int k = job.k0; k < job.k1; k++) {
+                if (round > 0 && !(ok = warp_wait(&sh.c_empty[s], (round - 1) & 1, &sh.failed))) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&sh.c_full[s], kCodes + (in ? kStep * 4 : 0));
+                    tma_load_2d(ring_c + s * kCodes, &p.codes, &sh.c_full[s], c0, t * kStep);
+                    if (in) bulk_load(ring_s + s * kStep, p.scales + ((size_t)(c0 >> 7) * p.rows_pad + (size_t)t * kStep) * 4, kStep * 4, &sh.c_full[s]);
+                }
+                __syncwarp();
+                if (++t == p.row_steps) t = 0;
+                if (++s == kC) { s = 0; round++; }
             }
-            __syncwarp();
-            if (++s == T::kC) { s = 0; round++; }
         }
-    } else if (warp >= 4) {
-        const int d = warp - 4;
-        const uint32_t t = (uint32_t)((d & 1) * 32 + lane), blk = (uint32_t)d >> 1;       // this thread's row of a step, and its 32 channels
-        // eight neighbouring lanes have eight rows of different index mod 8, so both swizzles spread them over all banks
-        const uint32_t src0 = t * 128 + (((2 * blk) ^ (t & 7)) << 4), src1 = t * 128 + (((2 * blk + 1) ^ (t & 7)) << 4);
-        const uint32_t dst_block = (blk >> 1) * kBlock + t * 128;
-        const uint32_t b_full0 = mapa_shared(smem_u32(&sh.b_full[0]), 0), d_empty0 = mapa_shared(smem_u32(&sh.d_empty), 0);
-        int sb = 0, sc = 0; uint32_t rb = 0, rc = 0, tiles_done = 0;
+      }
+    } else if (warp < 4 + kSummers) {
+        // sums: a warp holds 32 of the CTA's 128 output channels (its quarter of tensor memory) x 128 of the 256 input channels
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t tmem_mine = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+        const uint32_t d_empty0 = mapa_shared(smem_u32(&sh.d_empty[0]), 0);
+        uint32_t run = 0;
         bool ok = true;
-        for (int64_t it = from; it < to && ok;) {
-            const int tile = (int)(it / p.steps), k0 = (int)(it - (int64_t)tile * p.steps);
-            const int64_t tile_end = (int64_t)(tile + 1) * p.steps, end = tile_end < to ? tile_end : to;
-            const bool whole = k0 == 0 && end == tile_end;
-            const size_t slot = (size_t)pair * 2 + (it == from ? 0 : 1);
-            const int c0 = (tile % p.tiles_c) * kN, o0 = (tile / p.tiles_c) * 256 * GM;
-            for (int k = k0; it < end; it++, k++) {
-                const int row = (k % p.row_steps) * kStep + (int)t;
-                ok = warp_wait(&sh.c_full[sc], rc & 1, &sh.failed, false);
-                if (!ok) break;
-                const uint4 q0 = *reinterpret_cast<const uint4 *>(ring_c + sc * T::kCStage + src0), q1 = *reinterpret_cast<const uint4 *>(ring_c + sc * T::kCStage + src1);
-                // rows behind the last have codes 0 (the load fills them in) and no scale, channels behind the last likewise
-                uint32_t byte = (ring_s[sc * kStep + t] >> (8 * blk)) & 0xffu;
-                if (row >= p.rows || c0 + (int)rank * 128 + (int)blk * 32 >= p.cin) byte = 127u;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.c_empty[sc]);
-                if (rb > 0) ok = warp_wait(&sh.b_empty[sb], (rb - 1) & 1, &sh.failed, true);
-                if (!ok) break;
-                const uint32_t scale2 = byte << 7 | byte << 23;
-                uint8_t *dst = ring_b + sb * T::kBStage + dst_block;
-                const uint32_t w[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+        float sum[128];
+        while (ok && job.next()) {
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const uint2 a = decode4<CODE>(w[2 * j], scale2), b = decode4<CODE>(w[2 * j + 1], scale2);
-                    *reinterpret_cast<uint4 *>(dst + ((((blk & 1) * 4 + j) ^ (t & 7)) << 4)) = make_uint4(a.x, a.y, b.x, b.y);
+            for (int i = 0; i < 128; i++) sum[i] = 0.f;
+            for (int k = job.k0; k < job.k1; k += kRun, run++) {
+                const uint32_t buf = run & 1;
+                if (!(ok = warp_wait(&sh.d_full[buf], (run >> 1) & 1, &sh.failed))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) {
+                    float v[8];
+                    tmem_ld8(tmem_mine + buf * kN + c, v);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) sum[c + i] += v[i];
                 }
-                fence_proxy_async();
+                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(b_full0 + 8u * sb);
-                if (++sc == T::kC) { sc = 0; rc++; }
-                if (++sb == T::kB) { sb = 0; rb++; }
+                if (lane == 0) mbar_arrive_remote(d_empty0 + 8u * buf);
             }
-            if (!ok) break;
-            // the tile, or this pair's part of it: warp = 32 rows of output channels, every other 32 columns
-            ok = warp_wait(&sh.d_full, tiles_done & 1, &sh.failed, true);
-            if (!ok) break;
-            tc_fence_after();
-            const int quarter = warp & 3;
-#pragma unroll 1
-            for (int g = 0; g < GM; g++) {
-                const int r = g * 256 + (int)rank * 128 + quarter * 32 + lane, o = o0 + r;
-                float *out = whole ? p.dW + (size_t)o * p.cin + c0 : p.partial + slot * slot_floats(GM) + (size_t)r * kN;
-#pragma unroll 1
-                for (int c = (d >> 2) * 16; c < kN; c += 32) {
-                    if (c0 + c >= p.cin) break;                          // the same for the whole warp
-                    float v[16];
-                    tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(g * kN + c), v);
-                    if (o >= p.cout) continue;
-                    const int left = p.cin - c0 - c;
-                    if (whole && p.gamma) {
+            const int r = (int)rank * 128 + quarter * 32 + lane, o = (job.tile / p.tiles_c) * kM + r;
+            const int c0 = (job.tile % p.tiles_c) * kN + half * 128, left = ok && o < p.cout ? p.cin - c0 : 0;
+            const bool whole = job.slot < 0, vec = !whole || p.vec;
+            float *out = whole ? p.dW + (size_t)o * p.cin + c0 : p.partial + (size_t)job.slot * kSlot + (size_t)r * kN + half * 128;
+            const float *g = whole && p.gamma ? p.gamma + c0 : nullptr;
 #pragma unroll
-                        for (int i = 0; i < 16; i++) if (i < left) v[i] *= p.gamma[c0 + c + i];
+            for (int i = 0; i < 128; i += 4) {
+                if (i < left) {
+                    if (g) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) if (i + e < left) sum[i + e] *= g[i + e];
                     }
-                    if (left >= 16 && (!whole || p.vec)) {
+                    if (vec) *reinterpret_cast<float4 *>(out + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+                    else {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(out + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; i++) if (i < left) out[c + i] = v[i];
+                        for (int e = 0; e < 4; e++) if (i + e < left) out[i + e] = sum[i + e];
                     }
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(d_empty0);
-            tiles_done++;
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+        const int d = warp - 4 - kSummers;
+        // a step's 64 rows x 4 blocks of 32 channels: `sub` is half a column of them (32 rows, one per lane)
+        const int group = d / kGroupWarps, sub0 = d % kGroupWarps;
+        const uint32_t b_full0 = mapa_shared(smem_u32(&sh.b_full[0]), 0);
+        const uint32_t x7 = (uint32_t)lane & 7;
+        int sb = 0, sc = 0, turn = 0; uint32_t rb = 0, rc = 0;
+        bool ok = true;
+        while (ok && job.next()) {
+            int row = (job.k0 % p.row_steps) * kStep;
+            const int c0 = (job.tile % p.tiles_c) * kN + (int)rank * 128;
+            for (int k = job.k0; k < job.k1; k++) {
+                if (turn == group) {
+                    if (!(ok = warp_wait(&sh.c_full[sc], rc & 1, &sh.failed))) break;
+                    if (rb > 0 && !(ok = warp_wait(&sh.b_empty[sb], (rb - 1) & 1, &sh.failed))) break;
+                    const uint8_t *src = ring_c + sc * kCodes;
+                    uint8_t *dst = ring_b + sb * kOperand;
+#pragma unroll
+                    for (int i = 0; i < 8 / kGroupWarps; i++) {
+                        const int sub = sub0 + i * kGroupWarps;
+                        const uint32_t t = (uint32_t)((sub & 1) * 32 + lane), blk = (uint32_t)sub >> 1;
+                        // eight neighbouring lanes have eight rows of different index mod 8, so both swizzles spread them over all banks
+                        const uint4 q0 = *reinterpret_cast<const uint4 *>(src + t * 128 + (((2 * blk) ^ x7) << 4));
+                        const uint4 q1 = *reinterpret_cast<const uint4 *>(src + t * 128 + (((2 * blk + 1) ^ x7) << 4));
+                        // rows behind the last have codes 0 (the load fills them in) and no scale, channels behind the last likewise
+                        uint32_t byte = (ring_s[sc * kStep + t] >> (8 * blk)) & 0xffu;
+                        if (row + (int)t >= p.rows || c0 + (int)blk * 32 >= p.cin) byte = 127u;
+                        const uint32_t scale2 = byte << 7 | byte << 23;
+                        const uint32_t w[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+                        uint8_t *out = dst + (blk >> 1) * kBlock + t * 128;
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            *reinterpret_cast<uint4 *>(out + ((((blk & 1) * 4 + e) ^ x7) << 4)) =
+                                make_uint4(decode2<CODE>(w[2 * e], 0x4140, scale2), decode2<CODE>(w[2 * e], 0x4342, scale2),
+                                           decode2<CODE>(w[2 * e + 1], 0x4140, scale2), decode2<CODE>(w[2 * e + 1], 0x4342, scale2));
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(&sh.c_empty[sc]); mbar_arrive_remote(b_full0 + 8u * sb); }
+                }
+                if (++turn == kGroups) turn = 0;
+                if (++sc == kC) { sc = 0; rc++; }
+                if (++sb == kB) { sb = 0; rb++; }
+                row += kStep;
+                if (row >= p.row_steps * kStep) row = 0;
+            }
         }
     }
     tc_fence_before();
@@ -286,49 +325,39 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
     cluster_sync_all();      // neither CTA leaves, or frees tensor memory, while the other may still read its operands
     if (warp == 3) {
         tc_fence_after();
-        tmem2_dealloc(tmem, kCols);
+        tmem2_dealloc(tmem, 2 * kN);
     }
 }
 
 // dW of the tiles that several pairs have worked on: the parts in the order of their rows.  One CTA per 16 rows of a tile.
-template <int GM> __global__ void __launch_bounds__(256) wgrad8_sum_kernel(const __grid_constant__ Wgrad8Args p) {
+__global__ void __launch_bounds__(256) wgrad8_sum_kernel(const __grid_constant__ Wgrad8Args p) {
     pdl_enter();
-    const int tile = (int)blockIdx.x / (16 * GM), r0 = ((int)blockIdx.x % (16 * GM)) * 16;
-    const int64_t n = (int64_t)p.tiles * p.steps, begin = (int64_t)tile * p.steps, end = begin + p.steps;
+    const int t = (int)blockIdx.x / (kM / 16), r0 = ((int)blockIdx.x % (kM / 16)) * 16, tile = p.waves * p.pairs + t;
+    const int n = p.rest * p.steps, begin = t * p.steps, end = begin + p.steps;
     // the pair whose share holds step `begin`
-    int first = (int)(begin * p.pairs / n);
-    while (first > 0 && share(n, first, p.pairs) > begin) first--;
-    while (share(n, first + 1, p.pairs) <= begin) first++;
-    if (share(n, first + 1, p.pairs) >= end) return;                     // one pair: the tile is there already
-    const int c0 = (tile % p.tiles_c) * kN, o0 = (tile / p.tiles_c) * 256 * GM;
+    int first = (int)((int64_t)begin * p.sharers / n);
+    while (first > 0 && share(n, first, p.sharers) > begin) first--;
+    while (share(n, first + 1, p.sharers) <= begin) first++;
+    if (share(n, first + 1, p.sharers) >= end) return;                   // one pair: the tile is there already
+    const int c0 = (tile % p.tiles_c) * kN, o0 = (tile / p.tiles_c) * kM;
     const int c = (int)threadIdx.x & 63, row4 = (int)threadIdx.x >> 6;   // 4 columns of every fourth row
-    if (c0 + 4 * c >= p.cin) return;
     const int left = p.cin - c0 - 4 * c;
+    if (left <= 0) return;
     for (int r = r0 + row4; r < r0 + 16; r += 4) {
         const int o = o0 + r;
         if (o >= p.cout) return;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int q = first; q < p.pairs; q++) {
-            const int64_t start = share(n, q, p.pairs);
+        for (int q = first; q < p.sharers; q++) {
+            const int start = share(n, q, p.sharers);
             if (start >= end) break;
-            const size_t slot = (size_t)q * 2 + (start >= begin ? 0 : 1);
-            const float *src = p.partial + slot * slot_floats(GM) + (size_t)r * kN + 4 * c;
-            float4 v;
-            if (left >= 4) v = *reinterpret_cast<const float4 *>(src);
-            else v = make_float4(src[0], left > 1 ? src[1] : 0.f, left > 2 ? src[2] : 0.f, 0.f);
+            const float4 v = *reinterpret_cast<const float4 *>(p.partial + (size_t)(q * 2 + (start >= begin ? 0 : 1)) * kSlot + (size_t)r * kN + 4 * c);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
         float *out = p.dW + (size_t)o * p.cin + c0 + 4 * c;
         const float *g = p.gamma ? p.gamma + c0 + 4 * c : nullptr;
-        if (left >= 4) {
-            if (g) { s.x *= g[0]; s.y *= g[1]; s.z *= g[2]; s.w *= g[3]; }
-            if (p.vec) *reinterpret_cast<float4 *>(out) = s;
-            else { out[0] = s.x; out[1] = s.y; out[2] = s.z; out[3] = s.w; }
-        } else {
-            out[0] = g ? s.x * g[0] : s.x;
-            if (left > 1) out[1] = g ? s.y * g[1] : s.y;
-            if (left > 2) out[2] = g ? s.z * g[2] : s.z;
-        }
+        if (g) { s.x *= g[0]; if (left > 1) s.y *= g[1]; if (left > 2) s.z *= g[2]; if (left > 3) s.w *= g[3]; }
+        if (left > 3 && p.vec) *reinterpret_cast<float4 *>(out) = s;
+        else { out[0] = s.x; if (left > 1) out[1] = s.y; if (left > 2) out[2] = s.z; if (left > 3) out[3] = s.w; }
     }
 }
 
@@ -371,28 +400,26 @@ template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(
 }
 
 struct Plan {
-    int gm, row_steps, steps, tiles_c, tiles, pairs;
-    bool prepared;                   // dy goes through the workspace
-    int pitch;
+    int row_steps, steps, tiles_c, tiles, pairs, waves, rest, sharers;
+    int pitch;                       // elements per row of the prepared dy
     size_t prepared_bytes, partial_bytes;
 };
 bool direct(const revnet_wgrad_desc &d) { return d.dy_dtype == REVNET_BF16 && d.ld_dy % 8 == 0; }
 Plan plan_of(const revnet_ctx *ctx, const revnet_wgrad_desc &d, bool prepared) {
     Plan w{};
-    w.gm = d.cout > 256 ? 2 : 1;
     w.row_steps = (int)((d.rows + kStep - 1) / kStep);
     w.steps = w.row_steps * (d.dy_dtype == REVNET_F32 ? 3 : 1);
     w.tiles_c = (d.cin + kN - 1) / kN;
-    w.tiles = w.tiles_c * ((d.cout + 256 * w.gm - 1) / (256 * w.gm));
-    const int64_t n = (int64_t)w.tiles * w.steps;
-    int64_t pairs = (n + kStepsMin - 1) / kStepsMin;
+    w.tiles = w.tiles_c * ((d.cout + kM - 1) / kM);
     const int most = ctx->sm_count / 2;
-    w.pairs = (int)(pairs > most ? most : pairs);
-    w.prepared = prepared;
+    auto sharers_of = [&](int64_t tiles) { const int64_t q = (tiles * w.steps + kStepsMin - 1) / kStepsMin; return (int)(q < most ? q : most); };
+    w.pairs = sharers_of(w.tiles);
+    w.waves = w.pairs ? w.tiles / w.pairs : 0;
+    w.rest = w.tiles - w.waves * w.pairs;
+    w.sharers = sharers_of(w.rest);
     w.pitch = (d.cout + 7) & ~7;
     w.prepared_bytes = prepared ? ((size_t)w.steps * kStep * w.pitch * 2 + 255) & ~size_t(255) : 0;
-    w.partial_bytes = w.pairs == 0 || w.tiles % w.pairs == 0 ? 0 :          // whole tiles for every pair: no parts
-                      (size_t)w.pairs * 2 * w.gm * 256 * kN * 4;
+    w.partial_bytes = w.rest == 0 || w.rest % w.sharers == 0 ? 0 : (size_t)w.sharers * 2 * kSlot * 4;        // (a multiple: whole tiles for all of them)
     return w;
 }
 
@@ -405,11 +432,17 @@ bool encode_2d(void *fn, CUtensorMap *map, CUtensorMapDataType type, const void 
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int GM, int CODE> void run_t(Exec &ex, const Wgrad8Args &a, double bytes, double flops) {
+template <int CODE> void run_t(Exec &ex, const Wgrad8Args &a, double bytes, double flops) {
     static OncePerDevice once;
-    if (once.first(ex.ctx->device))
-        cudaFuncSetAttribute(wgrad8_kernel<GM, CODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<GM>::kSmem);
-    launch_cluster(ex, wgrad8_kernel<GM, CODE>, (unsigned)a.pairs * 2, kThreads, Tile<GM>::kSmem, 2, a);
+    if (once.first(ex.ctx->device)) cudaFuncSetAttribute(wgrad8_kernel<CODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    // the split of the registers adds up to what a launch gets with kRegs per thread, no more: a kernel built with fewer would wait for ever
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, wgrad8_kernel<CODE>) != cudaSuccess || attr.numRegs != kRegs) {
+        cudaGetLastError();
+        ex.failed = true; ex.ctx->err = "revnet_linear_wgrad: the kernel was built with another number of registers";
+        return;
+    }
+    launch_cluster(ex, wgrad8_kernel<CODE>, (unsigned)a.pairs * 2, kThreads, kSmem, 2, a);
     ex.check("wgrad8", bytes, flops);
 }
 
@@ -428,8 +461,8 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     const Checkpoint c = ck_view(ck, d.rows, d.cin);
     Wgrad8Args a{};
     a.scales = c.scales; a.gamma = gamma; a.dW = dW; a.partial = (float *)(workspace + w.prepared_bytes); a.status = ex.ctx->dev_status;
-    a.rows = (int)d.rows; a.cin = d.cin; a.cout = d.cout; a.row_steps = w.row_steps; a.steps = w.steps; a.tiles_c = w.tiles_c; a.tiles = w.tiles;
-    a.pairs = w.pairs; a.rows_pad = c.rows_pad; a.vec = d.cin % 4 == 0;
+    a.rows = (int)d.rows; a.cin = d.cin; a.cout = d.cout; a.row_steps = w.row_steps; a.steps = w.steps; a.tiles_c = w.tiles_c;
+    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = d.cin % 4 == 0;
     const int rows_step = w.row_steps * kStep;
     if (prepared) {
         const uint32_t groups = (uint32_t)w.pitch / 8;
@@ -449,11 +482,10 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
         return;
     }
     const double bytes = (double)d.rows * (2.0 * d.cout * (w.steps / w.row_steps) + d.cin) + 4.0 * d.cin * d.cout, flops = 2.0 * w.steps * kStep * d.cin * d.cout;
-    if (w.gm == 2) { if (d.code == REVNET_INT8) run_t<2, REVNET_INT8>(ex, a, bytes, flops); else run_t<2, REVNET_E4M3>(ex, a, bytes, flops); }
-    else { if (d.code == REVNET_INT8) run_t<1, REVNET_INT8>(ex, a, bytes, flops); else run_t<1, REVNET_E4M3>(ex, a, bytes, flops); }
+    if (d.code == REVNET_INT8) run_t<REVNET_INT8>(ex, a, bytes, flops);
+    else run_t<REVNET_E4M3>(ex, a, bytes, flops);
     if (w.partial_bytes) {
-        if (w.gm == 2) launch(ex, wgrad8_sum_kernel<2>, (unsigned)w.tiles * 32, 256, 0, a);
-        else launch(ex, wgrad8_sum_kernel<1>, (unsigned)w.tiles * 16, 256, 0, a);
+        launch(ex, wgrad8_sum_kernel, (unsigned)w.rest * (kM / 16), 256, 0, a);
         ex.check("wgrad8_sum", (double)w.partial_bytes);
     }
 }
