@@ -22,13 +22,16 @@ using namespace tc;
 
 constexpr int kThreads = 768;        // warp 0: dy loads, 1: MMAs, 2: codes, 3: tensor memory; 4..11: decoders, which also keep and store the sums
 constexpr int kSummers = 8, kDecoders = 12;
-constexpr int kGroups = 3, kGroupWarps = kDecoders / kGroups;    // every kGroups-th step is decoded by the same kGroupWarps warps
+constexpr int kGroups = 6, kGroupWarps = kDecoders / kGroups;    // every kGroups-th step is decoded by the same kGroupWarps warps
 constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
 static_assert((4 + kDecoders) * kRegsFew + kSummers * kRegsSums == kThreads / 32 * kRegs, "the split is the launch's total");
 constexpr int kStep = 64;            // rows per step
 constexpr int kRun = 16;             // steps per run of the tensor cores' own sum
 constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
+constexpr int kMaxPairs = 80;
 constexpr int kStepsMin = 8;         // a pair's share is at least that long where the work allows: shorter ones do not pay for their sums
+constexpr int kSplitSteps = 32;      // tiles are cut only where that saves as many steps: parts have to be written, read and added (8192 rows, 4096 x 1024:
+                                     // 78 us cut, 62 whole)
 constexpr uint32_t kBlock = 64 * 128;        // bytes of 64 rows x 64 channels of bf16, the unit of both operands
 constexpr int kA = 5, kB = 6, kC = 6;        // stages of the rings: dy, decoded x, codes
 // A group meets every phase of the barriers that it waits on only if a stage is always the same group's: else it could take the phase before the
@@ -55,12 +58,11 @@ struct alignas(64) Wgrad8Args {
     int tiles_c;                     // tiles along the input channels
     int pairs, waves;                // every pair takes `waves` whole tiles
     int rest, sharers;               // tiles left over, and how many pairs share their steps
+    int begin[kMaxPairs + 1];        // first of the steps left over that pair q works on (below 2^31: at most 79 tiles of fewer than 3 * 2^23 steps)
+    uint8_t first[kMaxPairs], last[kMaxPairs];       // of a tile left over: the pairs that work on it
     uint32_t rows_pad;
-    int vec;                         // dW rows take 16-byte stores
+    int vec;                         // dW rows take stores of 32 (2) or 16 bytes (1)
 };
-// first step of pair q's share of the n steps left over (fewer than 74 tiles of fewer than 3 * 2^23 steps: below 2^31)
-__host__ __device__ __forceinline__ int share(int n, int q, int sharers) { return (int)((int64_t)n * q / sharers); }
-
 // The pieces of work of a pair, in order; every role of both CTAs walks the same list.
 struct Pieces {
     const Wgrad8Args &p;
@@ -68,8 +70,7 @@ struct Pieces {
     int from = 0, it = 0, to = 0;
     int tile, k0, k1, slot;          // steps [k0, k1) of a tile; slot: where a part of a tile goes, -1 for a whole one
     __device__ __forceinline__ Pieces(const Wgrad8Args &a, int q) : p(a), pair(q) {
-        const int n = a.rest * a.steps;
-        if (q < a.sharers) { from = it = share(n, q, a.sharers); to = share(n, q + 1, a.sharers); }
+        if (q < a.sharers) { from = it = a.begin[q]; to = a.begin[q + 1]; }
     }
     __device__ __forceinline__ bool next() {
         if (wave < p.waves) { tile = pair + wave++ * p.pairs; k0 = 0; k1 = p.steps; slot = -1; return true; }
@@ -245,22 +246,34 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
             }
             const int r = (int)rank * 128 + quarter * 32 + lane, o = (job.tile / p.tiles_c) * kM + r;
             const int c0 = (job.tile % p.tiles_c) * kN + half * 128, left = ok && o < p.cout ? p.cin - c0 : 0;
-            const bool whole = job.slot < 0, vec = !whole || p.vec;
-            float *out = whole ? p.dW + (size_t)o * p.cin + c0 : p.partial + (size_t)job.slot * kSlot + (size_t)r * kN + half * 128;
-            const float *g = whole && p.gamma ? p.gamma + c0 : nullptr;
+            if (job.slot >= 0) {
+                // a part: [column quad][row][4], so that a warp's 32 rows are one run of 512 bytes
+                float4 *part = reinterpret_cast<float4 *>(p.partial + (size_t)job.slot * kSlot) + (size_t)half * 32 * kM + r;
 #pragma unroll
-            for (int i = 0; i < 128; i += 4) {
-                if (i < left) {
-                    if (g) {
+                for (int i = 0; i < 128; i += 4)
+                    if (i < left) part[(size_t)(i / 4) * kM] = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+                continue;
+            }
+            float *out = p.dW + (size_t)o * p.cin + c0;
+            if (p.gamma) {
+                const float *g = p.gamma + c0;
 #pragma unroll
-                        for (int e = 0; e < 4; e++) if (i + e < left) sum[i + e] *= g[i + e];
-                    }
-                    if (vec) *reinterpret_cast<float4 *>(out + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
-                    else {
+                for (int i = 0; i < 128; i++) if (i < left) sum[i] *= g[i];
+            }
+            if (p.vec == 2 && left >= 128) {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) if (i + e < left) out[i + e] = sum[i + e];
-                    }
+                for (int i = 0; i < 128; i += 8) {
+                    uint32_t t[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) t[e] = __float_as_uint(sum[i + e]);
+                    st8(out + i, t, true);
                 }
+            } else if (p.vec) {
+#pragma unroll
+                for (int i = 0; i < 128; i += 4) if (i < left) *reinterpret_cast<float4 *>(out + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 128; i++) if (i < left) out[i] = sum[i];
             }
         }
     } else {
@@ -329,36 +342,49 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
     }
 }
 
-// dW of the tiles that several pairs have worked on: the parts in the order of their rows.  One CTA per 16 rows of a tile.
-__global__ void __launch_bounds__(256) wgrad8_sum_kernel(const __grid_constant__ Wgrad8Args p) {
+// dW of the tiles that several pairs have worked on: the parts in a fixed order.  A CTA takes 8 rows x QUADS * 4 columns; LANES threads per quad
+// add every LANES-th part (and one of them then their sums), which a tile cut into many parts needs: 16384 rows, 256 x 256, 74 parts: 57 us with one.
+template <int LANES, int QUADS> __global__ void __launch_bounds__(8 * QUADS * LANES) wgrad8_sum_kernel(const __grid_constant__ Wgrad8Args p) {
+    __shared__ float4 sm[LANES == 1 ? 1 : LANES][8 * QUADS];
     pdl_enter();
-    const int t = (int)blockIdx.x / (kM / 16), r0 = ((int)blockIdx.x % (kM / 16)) * 16, tile = p.waves * p.pairs + t;
-    const int n = p.rest * p.steps, begin = t * p.steps, end = begin + p.steps;
-    // the pair whose share holds step `begin`
-    int first = (int)((int64_t)begin * p.sharers / n);
-    while (first > 0 && share(n, first, p.sharers) > begin) first--;
-    while (share(n, first + 1, p.sharers) <= begin) first++;
-    if (share(n, first + 1, p.sharers) >= end) return;                   // one pair: the tile is there already
-    const int c0 = (tile % p.tiles_c) * kN, o0 = (tile / p.tiles_c) * kM;
-    const int c = (int)threadIdx.x & 63, row4 = (int)threadIdx.x >> 6;   // 4 columns of every fourth row
-    const int left = p.cin - c0 - 4 * c;
-    if (left <= 0) return;
-    for (int r = r0 + row4; r < r0 + 16; r += 4) {
-        const int o = o0 + r;
-        if (o >= p.cout) return;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int q = first; q < p.sharers; q++) {
-            const int start = share(n, q, p.sharers);
-            if (start >= end) break;
-            const float4 v = *reinterpret_cast<const float4 *>(p.partial + (size_t)(q * 2 + (start >= begin ? 0 : 1)) * kSlot + (size_t)r * kN + 4 * c);
+    constexpr int kPer = (kM / 8) * (kN / 4 / QUADS);                    // CTAs per tile
+    const int t = (int)blockIdx.x / kPer, within = (int)blockIdx.x % kPer, tile = p.waves * p.pairs + t;
+    const int first = p.first[t], last = p.last[t];
+    if (first == last) return;                                           // one pair: the tile is there already
+    const int item = (int)threadIdx.x % (8 * QUADS), lane = (int)threadIdx.x / (8 * QUADS);
+    const int r = (within % (kM / 8)) * 8 + (item & 7), c = (within / (kM / 8)) * QUADS + (item >> 3);
+    const int o = (tile / p.tiles_c) * kM + r, ch = (tile % p.tiles_c) * kN + 4 * c, left = o < p.cout ? p.cin - ch : 0;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (left > 0) {
+#pragma unroll 4
+        for (int q = first + lane; q <= last; q += LANES) {
+            // the first pair's share may have begun before this tile: it is then the second part of that pair
+            const size_t slot = (size_t)q * 2 + (q > first || p.begin[q] >= t * p.steps ? 0 : 1);
+            const float4 v = reinterpret_cast<const float4 *>(p.partial + slot * kSlot)[(size_t)c * kM + r];
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
-        float *out = p.dW + (size_t)o * p.cin + c0 + 4 * c;
-        const float *g = p.gamma ? p.gamma + c0 + 4 * c : nullptr;
-        if (g) { s.x *= g[0]; if (left > 1) s.y *= g[1]; if (left > 2) s.z *= g[2]; if (left > 3) s.w *= g[3]; }
-        if (left > 3 && p.vec) *reinterpret_cast<float4 *>(out) = s;
-        else { out[0] = s.x; if (left > 1) out[1] = s.y; if (left > 2) out[2] = s.z; if (left > 3) out[3] = s.w; }
     }
+    if constexpr (LANES > 1) {
+        sm[lane][item] = s;
+        __syncthreads();
+        if (lane) return;
+#pragma unroll
+        for (int l = 1; l < LANES; l++) { const float4 v = sm[l][item]; s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; }
+    }
+    if (left <= 0) return;
+    float *out = p.dW + (size_t)o * p.cin + ch;
+    if (p.gamma) {
+        const float *g = p.gamma + ch;
+        s.x *= g[0];
+        if (left > 1) s.y *= g[1];
+        if (left > 2) s.z *= g[2];
+        if (left > 3) s.w *= g[3];
+    }
+    if (left > 3 && p.vec) *reinterpret_cast<float4 *>(out) = s;
+    else { out[0] = s.x; if (left > 1) out[1] = s.y; if (left > 2) out[2] = s.z; if (left > 3) out[3] = s.w; }
+}
+template <int LANES, int QUADS> void sum_t(Exec &ex, const Wgrad8Args &a) {
+    launch(ex, wgrad8_sum_kernel<LANES, QUADS>, (unsigned)a.rest * (kM / 8) * (kN / 4 / QUADS), 8 * QUADS * LANES, 0, a);
 }
 
 // dy for the loads: rows of `pitch` bf16 on 16-byte boundaries.  float32 becomes three parts, the bits of a value 8 at a time: their sum is the
@@ -411,12 +437,14 @@ Plan plan_of(const revnet_ctx *ctx, const revnet_wgrad_desc &d, bool prepared) {
     w.steps = w.row_steps * (d.dy_dtype == REVNET_F32 ? 3 : 1);
     w.tiles_c = (d.cin + kN - 1) / kN;
     w.tiles = w.tiles_c * ((d.cout + kM - 1) / kM);
-    const int most = ctx->sm_count / 2;
+    const int most = ctx->sm_count / 2 < kMaxPairs ? ctx->sm_count / 2 : kMaxPairs;
     auto sharers_of = [&](int64_t tiles) { const int64_t q = (tiles * w.steps + kStepsMin - 1) / kStepsMin; return (int)(q < most ? q : most); };
     w.pairs = sharers_of(w.tiles);
+    if (w.tiles < w.pairs && w.steps - (int64_t)w.tiles * w.steps / w.pairs < kSplitSteps) w.pairs = w.tiles;
     w.waves = w.pairs ? w.tiles / w.pairs : 0;
     w.rest = w.tiles - w.waves * w.pairs;
     w.sharers = sharers_of(w.rest);
+    if (w.rest && w.steps - (int64_t)w.rest * w.steps / w.sharers < kSplitSteps) w.sharers = w.rest;         // one more round of whole tiles
     w.pitch = (d.cout + 7) & ~7;
     w.prepared_bytes = prepared ? ((size_t)w.steps * kStep * w.pitch * 2 + 255) & ~size_t(255) : 0;
     w.partial_bytes = w.rest == 0 || w.rest % w.sharers == 0 ? 0 : (size_t)w.sharers * 2 * kSlot * 4;        // (a multiple: whole tiles for all of them)
@@ -462,7 +490,14 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     Wgrad8Args a{};
     a.scales = c.scales; a.gamma = gamma; a.dW = dW; a.partial = (float *)(workspace + w.prepared_bytes); a.status = ex.ctx->dev_status;
     a.rows = (int)d.rows; a.cin = d.cin; a.cout = d.cout; a.row_steps = w.row_steps; a.steps = w.steps; a.tiles_c = w.tiles_c;
-    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = d.cin % 4 == 0;
+    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = access_level(dW, d.cin, 4);
+    for (int q = 0; q <= w.sharers; q++) a.begin[q] = w.sharers ? (int)((int64_t)w.rest * w.steps * q / w.sharers) : 0;
+    for (int t = 0, q = 0; t < w.rest; t++) {
+        while (a.begin[q + 1] <= t * w.steps) q++;
+        a.first[t] = (uint8_t)q;
+        while (a.begin[q + 1] < (t + 1) * w.steps) q++;
+        a.last[t] = (uint8_t)q;
+    }
     const int rows_step = w.row_steps * kStep;
     if (prepared) {
         const uint32_t groups = (uint32_t)w.pitch / 8;
@@ -485,7 +520,9 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     if (d.code == REVNET_INT8) run_t<REVNET_INT8>(ex, a, bytes, flops);
     else run_t<REVNET_E4M3>(ex, a, bytes, flops);
     if (w.partial_bytes) {
-        launch(ex, wgrad8_sum_kernel, (unsigned)w.rest * (kM / 16), 256, 0, a);
+        if (w.sharers > 16 * w.rest) sum_t<16, 4>(ex, a);
+        else if (w.sharers > 3 * w.rest) sum_t<4, 8>(ex, a);
+        else sum_t<1, 32>(ex, a);
         ex.check("wgrad8_sum", (double)w.partial_bytes);
     }
 }
