@@ -2,9 +2,9 @@
 //
 //   store  ck = checkpoint of x, a = act(x)          load  a = act(x8)          bwd  dx = da act'(x8), checkpoint of act(x8)
 //
-// Every value is read and written once, so HBM bounds all of them.  A thread owns groups of 16 channels (see token.cuh): the amax of a block
-// of 32 is one shuffle between two lanes, no shared memory and no second pass.  Flat indexing over (row, group), since rows of any length
-// then leave no thread idle but in the last CTA.
+// Every value is read and written once, so HBM bounds all of them.  A thread owns 16 channels (token.cuh): consecutive ones where rows are
+// aligned whole blocks, the amax of a block of 32 being one shuffle between two lanes; spread over a warp's 512 elsewhere.  No shared memory and no second
+// pass.  Flat indexing over (row, group), since rows of any length then leave no thread idle but in the last CTA.
 #include "token.cuh"
 #include <type_traits>
 
@@ -39,247 +39,222 @@ struct Act8Args {
     Checkpoint ck, out;              // of x; bwd: of act(x8)
     int channels, half;              // of x; of a when gated
     int64_t ld_x, ld_a;              // of x, a above
-    int lv_x, lv_a, lv_u;            // access levels (token.cuh); lv_u: of the second half of a gated row
-    uint32_t total;                  // groups in all
-    FastDiv per_row;                 // groups per row
+    uint32_t total;                  // groups (SPREAD: warps' 512 channels) in all
+    FastDiv per_row;                 // of a row
 };
-__device__ __forceinline__ int left(int channels, int ch) { return channels - ch; }
 
-// the group that thread i of the flat index works on; false behind the last one
-__device__ __forceinline__ bool place(const Act8Args &p, uint32_t i, size_t &row, int &ch) {
+// this thread's row and first channel; false behind the last row
+template <bool SPREAD> __device__ __forceinline__ bool place(const Act8Args &p, size_t &row, int &ch) {
+    const uint32_t i = (blockIdx.x * kThreads + threadIdx.x) / (SPREAD ? 32 : 1);
     uint32_t r, g;
     p.per_row.divmod(i < p.total ? i : p.total - 1, r, g);
     row = r;
-    ch = (int)g * kGroup;
+    ch = SPREAD ? (int)g * 512 + (int)(threadIdx.x & 31) : (int)g * kGroup;
     return i < p.total;
 }
 
-template <class T, int CODE, int ACT, bool WITH_A>
+template <bool SPREAD, class T, int CODE, int ACT, bool WITH_A>
 __global__ void __launch_bounds__(kThreads) act8_store_kernel(const Act8Args p) {
     pdl_enter();
     size_t row; int ch;
-    const bool live = place(p, blockIdx.x * kThreads + threadIdx.x, row, ch);
-    const int n = live ? left(p.channels, ch) : 0;
+    const bool live = place<SPREAD>(p, row, ch);
+    const int left = live ? p.channels - ch : 0;
     float v[16];
-    load16((const T *)p.x + row * p.ld_x + ch, n, p.lv_x, v);
-    keep16<CODE>(p.ck, row, ch, live, v);
+    load16<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, v);
+    keep16<SPREAD, CODE>(p.ck, row, ch, live, v);
     if constexpr (WITH_A) {
-        float a[16];
 #pragma unroll
-        for (int i = 0; i < 16; i++) a[i] = act<ACT>(v[i]);
-        store16((T *)p.a + row * p.ld_a + ch, n, p.lv_a, a);
+        for (int i = 0; i < 16; i++) v[i] = act<ACT>(v[i]);
+        store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, v);
     }
 }
-// gated, halves in whole blocks of 32: the thread that needs g and u for a encodes both
-template <class T, int CODE>
+// gated, halves in whole blocks of 32 (CODE -1: without the checkpoint, halves of any length): the thread that needs g and u for a encodes both
+template <bool SPREAD, class T, int CODE>
 __global__ void __launch_bounds__(kThreads) act8_store_gated_kernel(const Act8Args p) {
     pdl_enter();
     size_t row; int ch;
-    const bool live = place(p, blockIdx.x * kThreads + threadIdx.x, row, ch);
-    const int n = live ? left(p.half, ch) : 0;
+    const bool live = place<SPREAD>(p, row, ch);
+    const int left = live ? p.half - ch : 0;
     float g[16], u[16];
     Raw16<T> rg, ru;
     const T *x = (const T *)p.x + row * p.ld_x + ch;
-    load_raw(x, n, p.lv_x, rg);
-    load_raw(x + p.half, n, p.lv_u, ru);
+    load_raw<SPREAD>(x, left, rg);
+    load_raw<SPREAD>(x + p.half, left, ru);
     unpack(rg, g); unpack(ru, u);
-    keep16<CODE>(p.ck, row, ch, live, g);
-    keep16<CODE>(p.ck, row, ch + p.half, live, u);
+    if constexpr (CODE >= 0) {
+        keep16<SPREAD, CODE>(p.ck, row, ch, live, g, p.half);            // the first half ends where the second begins
+        keep16<SPREAD, CODE>(p.ck, row, ch + p.half, live, u);
+    }
 #pragma unroll
     for (int i = 0; i < 16; i++) g[i] = act<REVNET_ACT_SILU>(g[i]) * u[i];
-    store16((T *)p.a + row * p.ld_a + ch, n, p.lv_a, g);
-}
-// the gated activation alone, for halves that end inside a block
-template <class T>
-__global__ void __launch_bounds__(kThreads) act8_gate_kernel(const Act8Args p) {
-    pdl_enter();
-    size_t row; int ch;
-    const bool live = place(p, blockIdx.x * kThreads + threadIdx.x, row, ch);
-    const int n = live ? left(p.half, ch) : 0;
-    float g[16], u[16];
-    const T *x = (const T *)p.x + row * p.ld_x + ch;
-    load16(x, n, p.lv_x, g);
-    load16(x + p.half, n, p.lv_u, u);
-#pragma unroll
-    for (int i = 0; i < 16; i++) g[i] = act<REVNET_ACT_SILU>(g[i]) * u[i];
-    store16((T *)p.a + row * p.ld_a + ch, n, p.lv_a, g);
+    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, g);
 }
 
-// 16 channels of the second half: where the half is no multiple of 16 their codes are not aligned and may have two scales
-template <int CODE> __device__ __forceinline__ void read_up(const Act8Args &p, size_t row, int ch, int n, float (&u)[16]) {
-    const int c0 = p.half + ch;
-    if ((p.half & 15) == 0 && n > 0) {
-        read16<CODE>(p.ck, row, c0, u);
-        return;
-    }
-    const uint8_t *codes = p.ck.codes + row * p.ck.pitch + c0;
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        u[i] = 0.f;
-        if (i < n) {
-            float t[16];
-            decode16<CODE>(make_uint4(codes[i], 0u, 0u, 0u), byte_of(p.ck.scales + scale_index(p.ck, row, c0 + i)), t);
-            u[i] = t[0];
-        }
-    }
-}
-
-template <class T, int CODE, int ACT>
+template <bool SPREAD, class T, int CODE, int ACT>
 __global__ void __launch_bounds__(kThreads) act8_load_kernel(const Act8Args p) {
     pdl_enter();
     size_t row; int ch;
-    if (!place(p, blockIdx.x * kThreads + threadIdx.x, row, ch)) return;
-    const int n = left(p.half, ch);
-    if (n <= 0) return;                              // the second group of a padded block
+    if (!place<SPREAD>(p, row, ch)) return;
+    const int left = p.half - ch;
+    if (left <= 0) return;                           // the second group of a padded block
     float v[16];
-    read16<CODE>(p.ck, row, ch, v);
+    RawCodes<SPREAD> rv, ru;
+    load_codes<SPREAD>(p.ck, row, ch, left, rv);
     if constexpr (ACT == REVNET_ACT_SWIGLU) {
         float u[16];
-        read_up<CODE>(p, row, ch, n, u);
+        load_codes<SPREAD>(p.ck, row, p.half + ch, left, ru);
+        decode<SPREAD, CODE>(rv, v);
+        decode<SPREAD, CODE>(ru, u);
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = act<REVNET_ACT_SILU>(v[i]) * u[i];
     } else {
+        decode<SPREAD, CODE>(rv, v);
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = act<ACT>(v[i]);
     }
-    store16((T *)p.a + row * p.ld_a + ch, n, p.lv_a, v);
+    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, v);
 }
 
-template <class T, int CODE, int ACT>
+template <bool SPREAD, class T, int CODE, int ACT>
 __global__ void __launch_bounds__(kThreads) act8_bwd_kernel(const Act8Args p) {
     pdl_enter();
     size_t row; int ch;
-    const bool live = place(p, blockIdx.x * kThreads + threadIdx.x, row, ch);
-    const int n = live ? left(p.half, ch) : 0;
-    float x[16], da[16], a[16];
-    load16((const T *)p.x + row * p.ld_x + ch, n, p.lv_x, da);
-    read16<CODE>(p.ck, row, ch, x);                  // codes of a padded row end are zeros
+    const bool live = place<SPREAD>(p, row, ch);
+    const int left = live ? p.half - ch : 0;
+    float x[16], da[16];
+    Raw16<T> rd;
+    RawCodes<SPREAD> rx, ru;
+    load_raw<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, rd);
+    load_codes<SPREAD>(p.ck, row, ch, left, rx);
+    if constexpr (ACT == REVNET_ACT_SWIGLU) load_codes<SPREAD>(p.ck, row, p.half + ch, left, ru);
+    unpack(rd, da);
+    decode<SPREAD, CODE>(rx, x);
     T *dx = (T *)p.a + row * p.ld_a + ch;
     if constexpr (ACT == REVNET_ACT_SWIGLU) {
-        float u[16], du[16];
-        read_up<CODE>(p, row, ch, n, u);
+        float u[16];
+        decode<SPREAD, CODE>(ru, u);
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             float s, d;
             act_grad<REVNET_ACT_SILU>(x[i], s, d);
-            a[i] = i < n ? s * u[i] : 0.f;           // behind the half's end x and u are the neighbours' values
-            du[i] = da[i] * s;
             x[i] = da[i] * u[i] * d;
+            u[i] *= s;                               // (codes that were not loaded are zeros, as the padding of the checkpoint has to be)
+            da[i] *= s;
         }
-        store16(dx, n, p.lv_a, x);
-        store16(dx + p.half, n, p.lv_u, du);
+        store16<SPREAD>(dx, left, x);
+        store16<SPREAD>(dx + p.half, left, da);
+        if (p.out.codes) keep16<SPREAD, CODE>(p.out, row, ch, live, u);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            float d;
-            act_grad<ACT>(x[i], a[i], d);
-            x[i] = ACT == REVNET_ACT_RELU && d == 0.f ? 0.f : da[i] * d;      // an infinite gradient stops at a closed ReLU too
+            float a, d;
+            act_grad<ACT>(x[i], a, d);
+            da[i] = ACT == REVNET_ACT_RELU && !(x[i] > 0.f) && x[i] == x[i] ? 0.f : da[i] * d;      // an infinite gradient stops at a closed ReLU too
+            x[i] = a;
         }
-        store16(dx, n, p.lv_a, x);
+        store16<SPREAD>(dx, left, da);
+        if (p.out.codes) keep16<SPREAD, CODE>(p.out, row, ch, live, x);
     }
-    if (p.out.codes) keep16<CODE>(p.out, row, ch, live, a);
 }
 
-bool fill(Act8Args &p, const revnet_act_desc &d, int channels_per_row) {
-    const bool gated = d.act == REVNET_ACT_SWIGLU;
+// channels_per_row: of the tensor that the threads walk along, padded to whole blocks
+bool fill(Act8Args &p, const revnet_act_desc &d, int channels_per_row, bool spread) {
     p.channels = d.channels;
-    p.half = gated ? d.channels / 2 : d.channels;
-    const uint32_t per_row = (uint32_t)ck_pitch(channels_per_row) / kGroup;
+    p.half = d.act == REVNET_ACT_SWIGLU ? d.channels / 2 : d.channels;
+    const uint32_t per_row = spread ? (uint32_t)(channels_per_row + 511) / 512 : (uint32_t)ck_pitch(channels_per_row) / kGroup;
     p.per_row = fast_div(per_row);
     p.total = (uint32_t)d.rows * per_row;            // the entry points keep it below 2^31
     return p.total > 0;
 }
-unsigned blocks(const Act8Args &p) { return (p.total + kThreads - 1) / kThreads; }
-int upper_level(const void *x, int64_t ld, int half, int size) { return access_level((const char *)x + (size_t)half * size, ld, size); }
-
-template <class T, int CODE> void store_t(Exec &ex, Act8Args p, const revnet_act_desc &d, double bytes) {
-    const unsigned g = blocks(p);
-    if (!p.a) launch_stream(ex, bytes, 0, act8_store_kernel<T, CODE, REVNET_ACT_NONE, false>, g, kThreads, 0, p);
-    else if (d.act == REVNET_ACT_NONE) launch_stream(ex, bytes, 0, act8_store_kernel<T, CODE, REVNET_ACT_NONE, true>, g, kThreads, 0, p);
-    else if (d.act == REVNET_ACT_RELU) launch_stream(ex, bytes, 0, act8_store_kernel<T, CODE, REVNET_ACT_RELU, true>, g, kThreads, 0, p);
-    else if (d.act == REVNET_ACT_GELU) launch_stream(ex, bytes, 0, act8_store_kernel<T, CODE, REVNET_ACT_GELU, true>, g, kThreads, 0, p);
-    else launch_stream(ex, bytes, 0, act8_store_kernel<T, CODE, REVNET_ACT_SILU, true>, g, kThreads, 0, p);
+template <bool SPREAD> unsigned blocks(const Act8Args &p) { return (unsigned)(((uint64_t)p.total * (SPREAD ? 32 : 1) + kThreads - 1) / kThreads); }
+template <bool SPREAD, class T, int CODE> void store_t(Exec &ex, const Act8Args &p, const revnet_act_desc &d, double bytes) {
+    const unsigned g = blocks<SPREAD>(p);
+    if (!p.a) launch_stream(ex, bytes, 0, act8_store_kernel<SPREAD, T, CODE, REVNET_ACT_NONE, false>, g, kThreads, 0, p);
+    else switch (d.act) {
+        case REVNET_ACT_NONE: launch_stream(ex, bytes, 0, act8_store_kernel<SPREAD, T, CODE, REVNET_ACT_NONE, true>, g, kThreads, 0, p); break;
+        case REVNET_ACT_RELU: launch_stream(ex, bytes, 0, act8_store_kernel<SPREAD, T, CODE, REVNET_ACT_RELU, true>, g, kThreads, 0, p); break;
+        case REVNET_ACT_GELU: launch_stream(ex, bytes, 0, act8_store_kernel<SPREAD, T, CODE, REVNET_ACT_GELU, true>, g, kThreads, 0, p); break;
+        case REVNET_ACT_SILU: launch_stream(ex, bytes, 0, act8_store_kernel<SPREAD, T, CODE, REVNET_ACT_SILU, true>, g, kThreads, 0, p); break;
+        default: launch_stream(ex, bytes, 0, act8_store_gated_kernel<SPREAD, T, CODE>, g, kThreads, 0, p); break;
+    }
     ex.check("act8_store", bytes);
 }
-template <class T, int CODE> void load_t(Exec &ex, const Act8Args &p, const revnet_act_desc &d, double bytes) {
-    const unsigned g = blocks(p);
+template <bool SPREAD, class T, int CODE> void load_t(Exec &ex, const Act8Args &p, const revnet_act_desc &d, double bytes) {
+    const unsigned g = blocks<SPREAD>(p);
     switch (d.act) {
-        case REVNET_ACT_NONE: launch_stream(ex, bytes, 0, act8_load_kernel<T, CODE, REVNET_ACT_NONE>, g, kThreads, 0, p); break;
-        case REVNET_ACT_RELU: launch_stream(ex, bytes, 0, act8_load_kernel<T, CODE, REVNET_ACT_RELU>, g, kThreads, 0, p); break;
-        case REVNET_ACT_GELU: launch_stream(ex, bytes, 0, act8_load_kernel<T, CODE, REVNET_ACT_GELU>, g, kThreads, 0, p); break;
-        case REVNET_ACT_SILU: launch_stream(ex, bytes, 0, act8_load_kernel<T, CODE, REVNET_ACT_SILU>, g, kThreads, 0, p); break;
-        default: launch_stream(ex, bytes, 0, act8_load_kernel<T, CODE, REVNET_ACT_SWIGLU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_NONE: launch_stream(ex, bytes, 0, act8_load_kernel<SPREAD, T, CODE, REVNET_ACT_NONE>, g, kThreads, 0, p); break;
+        case REVNET_ACT_RELU: launch_stream(ex, bytes, 0, act8_load_kernel<SPREAD, T, CODE, REVNET_ACT_RELU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_GELU: launch_stream(ex, bytes, 0, act8_load_kernel<SPREAD, T, CODE, REVNET_ACT_GELU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_SILU: launch_stream(ex, bytes, 0, act8_load_kernel<SPREAD, T, CODE, REVNET_ACT_SILU>, g, kThreads, 0, p); break;
+        default: launch_stream(ex, bytes, 0, act8_load_kernel<SPREAD, T, CODE, REVNET_ACT_SWIGLU>, g, kThreads, 0, p); break;
     }
     ex.check("act8_load", bytes);
 }
-template <class T, int CODE> void bwd_t(Exec &ex, const Act8Args &p, const revnet_act_desc &d, double bytes) {
-    const unsigned g = blocks(p);
+template <bool SPREAD, class T, int CODE> void bwd_t(Exec &ex, const Act8Args &p, const revnet_act_desc &d, double bytes) {
+    const unsigned g = blocks<SPREAD>(p);
     switch (d.act) {
-        case REVNET_ACT_NONE: launch_stream(ex, bytes, 0, act8_bwd_kernel<T, CODE, REVNET_ACT_NONE>, g, kThreads, 0, p); break;
-        case REVNET_ACT_RELU: launch_stream(ex, bytes, 0, act8_bwd_kernel<T, CODE, REVNET_ACT_RELU>, g, kThreads, 0, p); break;
-        case REVNET_ACT_GELU: launch_stream(ex, bytes, 0, act8_bwd_kernel<T, CODE, REVNET_ACT_GELU>, g, kThreads, 0, p); break;
-        case REVNET_ACT_SILU: launch_stream(ex, bytes, 0, act8_bwd_kernel<T, CODE, REVNET_ACT_SILU>, g, kThreads, 0, p); break;
-        default: launch_stream(ex, bytes, 0, act8_bwd_kernel<T, CODE, REVNET_ACT_SWIGLU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_NONE: launch_stream(ex, bytes, 0, act8_bwd_kernel<SPREAD, T, CODE, REVNET_ACT_NONE>, g, kThreads, 0, p); break;
+        case REVNET_ACT_RELU: launch_stream(ex, bytes, 0, act8_bwd_kernel<SPREAD, T, CODE, REVNET_ACT_RELU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_GELU: launch_stream(ex, bytes, 0, act8_bwd_kernel<SPREAD, T, CODE, REVNET_ACT_GELU>, g, kThreads, 0, p); break;
+        case REVNET_ACT_SILU: launch_stream(ex, bytes, 0, act8_bwd_kernel<SPREAD, T, CODE, REVNET_ACT_SILU>, g, kThreads, 0, p); break;
+        default: launch_stream(ex, bytes, 0, act8_bwd_kernel<SPREAD, T, CODE, REVNET_ACT_SWIGLU>, g, kThreads, 0, p); break;
     }
     ex.check("act8_bwd", bytes);
 }
-template <class F> void by_type(const revnet_act_desc &d, F &&f) {
-    if (d.dtype == REVNET_F32) { if (d.code == REVNET_INT8) f(float(), std::integral_constant<int, REVNET_INT8>()); else f(float(), std::integral_constant<int, REVNET_E4M3>()); }
-    else { if (d.code == REVNET_INT8) f(bf16(), std::integral_constant<int, REVNET_INT8>()); else f(bf16(), std::integral_constant<int, REVNET_E4M3>()); }
+template <class F> void by_type(const revnet_act_desc &d, bool spread, F &&f) {
+    auto code = [&](auto s, auto t) {
+        if (d.code == REVNET_INT8) f(s, t, std::integral_constant<int, REVNET_INT8>());
+        else f(s, t, std::integral_constant<int, REVNET_E4M3>());
+    };
+    auto type = [&](auto s) { if (d.dtype == REVNET_F32) code(s, float()); else code(s, bf16()); };
+    if (spread) type(std::true_type()); else type(std::false_type());
 }
 
 }  // namespace
 
 void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a) {
-    const int size = d.dtype == REVNET_F32 ? 4 : 2;
-    const bool gated = d.act == REVNET_ACT_SWIGLU;
+    const int size = d.dtype == REVNET_F32 ? 4 : 2, half = d.channels / 2;
+    const bool gated = d.act == REVNET_ACT_SWIGLU && a;
     Act8Args p{};
     p.x = x; p.a = a; p.ck = ck_view(ck, d.rows, d.channels);
     p.ld_x = d.ld_x; p.ld_a = d.ld_a;
-    p.lv_x = access_level(x, d.ld_x, size); p.lv_a = access_level(a, d.ld_a, size);
-    p.lv_u = upper_level(x, d.ld_x, d.channels / 2, size);
     const double n = (double)d.rows * d.channels, out = a ? (gated ? n / 2 : n) * size : 0;
-    if (!(gated && a)) {
-        if (fill(p, d, d.channels)) by_type(d, [&](auto t, auto c) { store_t<decltype(t), decltype(c)::value>(ex, p, d, n * (size + 1) + out); });
+    const bool whole = rows_aligned(x, d.ld_x, size) && rows_aligned(a, d.ld_a, size) && (gated ? half : d.channels) % 32 == 0;
+    if (!gated || half % 32 == 0) {
+        if (!fill(p, d, gated ? half : d.channels, !whole)) return;
+        by_type(d, !whole, [&](auto s, auto t, auto c) { store_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, n * (size + 1) + out); });
         return;
     }
-    if (d.channels / 2 % 32 == 0) {
-        if (!fill(p, d, d.channels / 2)) return;
-        by_type(d, [&](auto t, auto c) {
-            launch_stream(ex, n * (size + 1) + out, 0, act8_store_gated_kernel<decltype(t), decltype(c)::value>, blocks(p), kThreads, 0, p);
-        });
-        ex.check("act8_store", n * (size + 1) + out);
-        return;
-    }
+    // halves that end inside a block: the checkpoint first, then the activation alone
     Act8Args only = p;
     only.a = nullptr;
-    if (!fill(only, d, d.channels)) return;
-    by_type(d, [&](auto t, auto c) { store_t<decltype(t), decltype(c)::value>(ex, only, d, n * (size + 1)); });
-    fill(p, d, d.channels / 2);
-    if (d.dtype == REVNET_F32) launch_stream(ex, n * size + out, 0, act8_gate_kernel<float>, blocks(p), kThreads, 0, p);
-    else launch_stream(ex, n * size + out, 0, act8_gate_kernel<bf16>, blocks(p), kThreads, 0, p);
+    const bool first = rows_aligned(x, d.ld_x, size) && d.channels % 32 == 0;
+    if (!fill(only, d, d.channels, !first)) return;
+    by_type(d, !first, [&](auto s, auto t, auto c) { store_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, only, d, n * (size + 1)); });
+    fill(p, d, half, true);
+    if (d.dtype == REVNET_F32) launch_stream(ex, n * size + out, 0, act8_store_gated_kernel<true, float, -1>, blocks<true>(p), kThreads, 0, p);
+    else launch_stream(ex, n * size + out, 0, act8_store_gated_kernel<true, bf16, -1>, blocks<true>(p), kThreads, 0, p);
     ex.check("act8_gate", n * size + out);
 }
 
 void act8_load(Exec &ex, const revnet_act_desc &d, const void *ck, void *a) {
-    const int size = d.dtype == REVNET_F32 ? 4 : 2;
+    const int size = d.dtype == REVNET_F32 ? 4 : 2, out = d.act == REVNET_ACT_SWIGLU ? d.channels / 2 : d.channels;
     Act8Args p{};
     p.a = a; p.ck = ck_view(ck, d.rows, d.channels);
-    p.ld_a = d.ld_a; p.lv_a = access_level(a, d.ld_a, size);
-    if (!fill(p, d, d.act == REVNET_ACT_SWIGLU ? d.channels / 2 : d.channels)) return;
+    p.ld_a = d.ld_a;
+    const bool whole = rows_aligned(a, d.ld_a, size) && out % 32 == 0;
+    if (!fill(p, d, out, !whole)) return;
     const double bytes = (double)d.rows * (d.channels + (double)p.half * size);
-    by_type(d, [&](auto t, auto c) { load_t<decltype(t), decltype(c)::value>(ex, p, d, bytes); });
+    by_type(d, !whole, [&](auto s, auto t, auto c) { load_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
 }
 
 void act8_bwd(Exec &ex, const revnet_act_desc &d, const void *ck, const void *da, void *dx, void *a_ck) {
-    const int size = d.dtype == REVNET_F32 ? 4 : 2;
-    const int out = d.act == REVNET_ACT_SWIGLU ? d.channels / 2 : d.channels;
+    const int size = d.dtype == REVNET_F32 ? 4 : 2, out = d.act == REVNET_ACT_SWIGLU ? d.channels / 2 : d.channels;
     Act8Args p{};
     p.x = da; p.a = dx; p.ck = ck_view(ck, d.rows, d.channels); p.out = ck_view(a_ck, d.rows, out);
     p.ld_x = d.ld_a; p.ld_a = d.ld_x;
-    p.lv_x = access_level(da, d.ld_a, size); p.lv_a = access_level(dx, d.ld_x, size);
-    p.lv_u = upper_level(dx, d.ld_x, d.channels / 2, size);
-    if (!fill(p, d, out)) return;
+    const bool whole = rows_aligned(da, d.ld_a, size) && rows_aligned(dx, d.ld_x, size) && out % 32 == 0;
+    if (!fill(p, d, out, !whole)) return;
     const double bytes = (double)d.rows * (d.channels * (1.0 + size) + out * (size + (a_ck ? 1.0 : 0.0)));
-    by_type(d, [&](auto t, auto c) { bwd_t<decltype(t), decltype(c)::value>(ex, p, d, bytes); });
+    by_type(d, !whole, [&](auto s, auto t, auto c) { bwd_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
 }

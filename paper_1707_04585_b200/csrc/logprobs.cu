@@ -7,8 +7,9 @@
 // rises; the threads' triples are joined at the end by the same rule.  With few rows a row is split over the CTAs of a cluster, which
 // join through distributed shared memory: no workspace, no second launch.
 // The k most likely tokens: every warp keeps a sorted list of its own, one entry per lane, of keys (logit, then the lower index) as 64-bit
-// integers.  A vector of logits is looked at again only if one of them reaches the list's last entry, which after the first few hundred
-// is rare in any order but an ascending one (n elements in random order change a list k ln(n / k) times).
+// integers.  A logit is looked at again only if it reaches the largest k-th entry of any list of the CTA, which after the first few hundred
+// is rare in any order but an ascending one (n elements in random order change a list k ln(n / k) times); the first bound is the k-th largest of
+// a warp's 32 lanes' maxima.  Leaving out what no list needs changes no result.
 // Rows need not be aligned: elements in front of the first 32-byte boundary and behind the last are read one by one.
 #include "token.cuh"
 #include <math.h>
@@ -48,11 +49,8 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
     rescale(b, m);
     return Sums{m, a.s + b.s, a.t + b.t};
 }
-// N logits
-template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N]) {
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < N; i++) top = fmaxf(top, x[i]);
+// N logits, top the largest of them
+template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N], float top) {
     top *= kLog2e;
     if (top > a.m) rescale(a, top);
     // (a.m stays -inf while every logit so far is: then all differences would be NaN)
@@ -64,34 +62,61 @@ template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N
         a.t = fmaf(fmaxf(d, -200.f), e, a.t);        // 0 log 0 = 0: e is 0 far before -200 (fmaxf also drops a NaN, which s carries)
     }
 }
+__device__ __forceinline__ float top_of(const Raw16<float> &r) {
+    float t = __uint_as_float(r.w[0]);
+#pragma unroll
+    for (int i = 1; i < 16; i++) t = fmaxf(t, __uint_as_float(r.w[i]));
+    return t;
+}
+__device__ __forceinline__ float top_of(const Raw16<bf16> &r) {
+    __nv_bfloat162 t = *reinterpret_cast<const __nv_bfloat162 *>(&r.w[0]);
+#pragma unroll
+    for (int i = 1; i < 8; i++) t = __hmax2(t, *reinterpret_cast<const __nv_bfloat162 *>(&r.w[i]));
+    return fmaxf(__low2float(t), __high2float(t));
+}
 
 // ---- most likely tokens
-__device__ __forceinline__ unsigned long long key_of(float x, int index) {
+// bits in the logits' order, NaN above all, never 0
+__device__ __forceinline__ uint32_t order_of(float x) {
     x += 0.f;                                        // -0 -> 0: equal logits are equal keys
-    uint32_t b = __float_as_uint(x);
-    b = x != x ? 0xffffffffu : (b & 0x80000000u ? ~b : b | 0x80000000u);
-    return (unsigned long long)b << 32 | (uint32_t)~index;
+    const uint32_t b = __float_as_uint(x);
+    return x != x ? 0xffffffffu : (b & 0x80000000u ? ~b : b | 0x80000000u);
 }
+__device__ __forceinline__ unsigned long long key_of(float x, int index) { return (unsigned long long)order_of(x) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ float value_of(unsigned long long key) {
     const uint32_t b = (uint32_t)(key >> 32);
     return b == 0xffffffffu ? NAN : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
-struct TopList {                     // lane i: the i-th largest key so far, 0 for none; last: the k-th
-    unsigned long long mine, last;
+struct TopList {                     // lane i: the i-th largest key so far, 0 for none; least: keys up to this one are not needed
+    unsigned long long mine, least;
     int k;
     __device__ __forceinline__ void offer(unsigned long long key) {       // one key per lane; the whole warp calls
-        unsigned todo = __ballot_sync(0xffffffffu, key > last);
+        unsigned todo = __ballot_sync(0xffffffffu, key > least);
         const int lane = threadIdx.x & 31;
         while (todo) {
             const int src = __ffs(todo) - 1;
             todo &= todo - 1;
             const unsigned long long c = __shfl_sync(0xffffffffu, key, src);
-            if (c <= last) continue;
+            if (c <= least) continue;
             const int at = __popc(__ballot_sync(0xffffffffu, mine > c));
             const unsigned long long up = __shfl_up_sync(0xffffffffu, mine, 1);
             mine = lane < at ? mine : (lane == at ? c : up);
-            last = __shfl_sync(0xffffffffu, mine, k - 1);
+            const unsigned long long kth = __shfl_sync(0xffffffffu, mine, k - 1);
+            if (kth > least) least = kth;
         }
+    }
+    // a first bound from one logit per lane (order 0: none): the k-th largest of the 32, below every key of that logit
+    __device__ __forceinline__ void bound(uint32_t order) {
+        const int lane = threadIdx.x & 31;
+        int rank = 0;
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+            const uint32_t o = __shfl_sync(0xffffffffu, order, j);
+            rank += o > order || (o == order && j < lane) ? 1 : 0;
+        }
+        const unsigned at = __ballot_sync(0xffffffffu, rank == k - 1);
+        const unsigned long long b = (unsigned long long)__shfl_sync(0xffffffffu, order, __ffs(at) - 1) << 32;
+        if (b > least) least = b;
     }
 };
 
@@ -120,7 +145,7 @@ constexpr int kVec = 16;             // logits per step of a thread
 template <class T, bool TOP, bool CLUSTER>
 __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
     __shared__ float sm_m[16], sm_s[16], sm_t[16];
-    __shared__ unsigned long long lists[TOP ? 16 * 32 : 1];
+    __shared__ unsigned long long lists[TOP ? 16 * 32 : 1], best;        // best: the largest k-th key of a warp's list
     pdl_enter();
     const uint32_t rank = CLUSTER ? cluster_rank() : 0, ctas = CLUSTER ? cluster_size() : 1;
     const size_t row = blockIdx.x / ctas;
@@ -134,27 +159,43 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
     const int vecs = (len - head) / kVec, tail0 = head + vecs * kVec;
     Sums sum{-INFINITY, 0.f, 0.f};
     TopList list{0ull, 0ull, p.k};
+    if (TOP) {
+        if (threadIdx.x == 0) best = 0ull;
+        __syncthreads();
+    }
 
-    // whole warps go round the loop: the list's shuffles need all lanes
+    // whole warps go round the loop: the list's shuffles need all lanes.  The next vector is on its way while one is worked on.
+    Raw16<T> raw, next;
+    if ((int)threadIdx.x < vecs) load_raw<false>(xb + head + (int)threadIdx.x * kVec, kVec, next);
     for (int v0 = warp * 32; v0 < vecs; v0 += blockDim.x) {
         const int v = v0 + lane;
         const bool ok = v < vecs;
+        raw = next;
+        if (v + (int)blockDim.x < vecs) load_raw<false>(xb + head + (v + (int)blockDim.x) * kVec, kVec, next);
         float f[kVec];
-        if (ok) load16(xb + head + v * kVec, kVec, 2, f);
-        else {
-#pragma unroll
-            for (int i = 0; i < kVec; i++) f[i] = -INFINITY;
-        }
-        if (ok) add(sum, f);
+        const float top = top_of(raw);
+        unpack(raw, f);
+        if (ok) add(sum, f, top);
         if constexpr (TOP) {
-            float top = f[0];
-            bool odd = f[0] != f[0];
+            const unsigned long long other = __shfl_sync(0xffffffffu, *(volatile unsigned long long *)&best, 0);
+            if (other > list.least) list.least = other;
+            const bool nan = sum.s != sum.s;                             // (one of this thread's logits so far)
+            if (list.least == 0ull) list.bound(ok ? (nan ? 1u : order_of(top)) : 0u);
+            bool look = ok && (nan || order_of(top) >= (uint32_t)(list.least >> 32));
+            if (__any_sync(0xffffffffu, look)) {
+                const float bar = list.least ? value_of(list.least) : -INFINITY;
+                uint32_t todo = 0;
+                if (look) {
 #pragma unroll
-            for (int i = 1; i < kVec; i++) { top = fmaxf(top, f[i]); odd |= f[i] != f[i]; }
-            const bool look = ok && (odd || key_of(top, 0) >= (list.last & 0xffffffff00000000ull));
-            if (__ballot_sync(0xffffffffu, look)) {
-#pragma unroll
-                for (int i = 0; i < kVec; i++) list.offer(look ? key_of(f[i], begin + head + v * kVec + i) : 0ull);
+                    for (int i = 0; i < kVec; i++) todo |= !(f[i] < bar) ? 1u << i : 0u;
+                }
+                while (__any_sync(0xffffffffu, todo != 0)) {
+                    const int i = begin + head + v * kVec + (todo ? __ffs(todo) - 1 : 0);
+                    list.offer(todo ? key_of(to_f(x[i]), i) : 0ull);
+                    todo &= todo - 1;
+                }
+                const unsigned long long kth = __shfl_sync(0xffffffffu, list.mine, p.k - 1);
+                if (lane == 0 && kth > other) atomicMax(&best, kth);
             }
         }
     }
@@ -163,7 +204,7 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
         const bool ok = e < head + len - tail0;
         const int i = e < head ? e : tail0 + e - head;
         const float f[1] = {ok ? to_f(xb[i]) : -INFINITY};
-        if (ok) add(sum, f);
+        if (ok) add(sum, f, f[0]);
         if constexpr (TOP) list.offer(ok ? key_of(f[0], begin + i) : 0ull);
     }
     for (int o = 16; o; o >>= 1) {
@@ -171,7 +212,7 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
         sum = join(sum, b);
     }
     if (lane == 0) { sm_m[warp] = sum.m; sm_s[warp] = sum.s; sm_t[warp] = sum.t; }
-    if constexpr (TOP) lists[warp * 32 + lane] = list.mine;
+    if constexpr (TOP) lists[warp * 32 + lane] = lane < p.k ? list.mine : 0ull;
     __syncthreads();
     if (warp == 0) {
         // lane w: the sums of warp w
@@ -181,8 +222,9 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
             sum = join(sum, b);
         }
         if constexpr (TOP) {
-            for (int w = 1; w < warps; w++) list.offer(lane < p.k ? lists[w * 32 + lane] : 0ull);
-            if (CLUSTER) { __syncwarp(); lists[lane] = list.mine; }
+            list.least = __shfl_sync(0xffffffffu, list.mine, p.k - 1);   // (the bound may be a key of another list)
+            for (int w = 1; w < warps; w++) list.offer(lists[w * 32 + lane]);
+            if (CLUSTER) { __syncwarp(); lists[lane] = lane < p.k ? list.mine : 0ull; }
         }
         if (CLUSTER && lane == 0) { sm_m[0] = sum.m; sm_s[0] = sum.s; sm_t[0] = sum.t; }
     }
@@ -195,7 +237,7 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
                 sum = join(sum, b);
             }
             if constexpr (TOP)
-                for (uint32_t c = 1; c < ctas; c++) list.offer(lane < p.k ? remote(&lists[lane], c) : 0ull);
+                for (uint32_t c = 1; c < ctas; c++) list.offer(remote(&lists[lane], c));
         }
         cluster_sync();              // nobody leaves while rank 0 reads
         if (rank != 0) return;
@@ -256,14 +298,14 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogpArgs p) {
     const int vecs = (len - head) / kVec, tail0 = head + vecs * kVec;
     for (int v = threadIdx.x; v < vecs; v += blockDim.x) {
         float f[kVec];
-        load16(x + head + v * kVec, kVec, 2, f);
+        load16<false>(x + head + v * kVec, kVec, f);
         const int at = tgt - (begin + head + v * kVec);
 #pragma unroll
         for (int i = 0; i < kVec; i++) {
             const float d = none ? 0.f : grad(f[i], lse, g, ge, ent2);
             f[i] = at == i && !none ? d + g : d;
         }
-        store16(dx + head + v * kVec, kVec, 2, f);
+        store16<false>(dx + head + v * kVec, kVec, f);
     }
     for (int e = threadIdx.x; e < head + len - tail0; e += blockDim.x) {
         const int i = e < head ? e : tail0 + e - head;
@@ -296,7 +338,7 @@ void logprobs_fwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, co
     while (threads < 512 && (int)threads * kVec < d.vocab) threads *= 2;
     // a row is split while its parts stay longer than one step of a CTA and the GPU has SMs to spare
     int cluster = 1;
-    while (cluster < 8 && d.rows * cluster * 2 <= 2 * ex.ctx->sm_count && d.vocab / (cluster * 2) >= (int)threads * kVec) cluster *= 2;
+    while (cluster < 8 && d.rows * cluster * 2 <= 4 * ex.ctx->sm_count && d.vocab / (cluster * 2) >= (int)threads * kVec) cluster *= 2;
     p.chunk = (d.vocab + cluster - 1) / cluster;
     const double bytes = (double)d.rows * d.vocab * (d.dtype == REVNET_F32 ? 4 : 2);
     if (d.dtype == REVNET_F32) fwd_t<float>(ex, p, cluster, threads);

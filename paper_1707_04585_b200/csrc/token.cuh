@@ -4,10 +4,6 @@
 #include "common.cuh"
 #include <cuda_fp8.h>
 
-// A thread's unit of work in the elementwise kernels is a group of 16 consecutive channels: 16 code bytes are one 16-byte access, 16 bf16
-// one of 32 bytes, and the two lanes 2i, 2i + 1 hold the 32 channels that share a scale.
-constexpr int kGroup = 16;
-
 // ---------------------------------------------------------------- host side
 struct Checkpoint {            // a checkpoint buffer taken apart
     uint8_t *codes, *scales;
@@ -23,12 +19,8 @@ static inline Checkpoint ck_view(const void *buf, int64_t rows, int channels) {
     uint8_t *b = (uint8_t *)buf;
     return Checkpoint{b, b ? b + ck_scales_at(rows, channels) : nullptr, ck_pitch(channels), (uint32_t)((rows + 63) & ~int64_t(63))};
 }
-// How wide a thread may access the rows of a tensor at p, `ld` elements of `size` bytes apart, at multiples of 16 channels:
-// 2: 32 bytes, 1: 16 bytes, 0: element by element.
-static inline int access_level(const void *p, int64_t ld, int size) {
-    const uint64_t a = (uint64_t)(uintptr_t)p | (uint64_t)ld * size;
-    return a % 32 == 0 ? 2 : (a % 16 == 0 ? 1 : 0);
-}
+// whether 32-byte accesses reach the rows of a tensor at p, `ld` elements of `size` bytes apart, at multiples of 16 channels (null: yes)
+static inline bool rows_aligned(const void *p, int64_t ld, int size) { return !p || (((uint64_t)(uintptr_t)p | (uint64_t)ld * size) & 31) == 0; }
 
 // ---------------------------------------------------------------- act8.cu, norm.cu, wgrad8.cu, logprobs.cu
 void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a);
@@ -59,36 +51,34 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t byte_of(const uint8_t *p) { return *p; }
 
+// A thread's 16 channels.  Rows of whole blocks of 32 on 32-byte boundaries: 16 consecutive ones, moved by wide accesses.  Any other rows
+// (SPREAD): every 32nd of 512, the lanes of a warp side by side, so that a warp's accesses are whole lines where a thread's would be an
+// element each.  `left` is the row's length minus the thread's first channel: at most 0, none of them exists; else, unless SPREAD, all do.
+constexpr int kGroup = 16;
+template <bool SPREAD> __device__ __forceinline__ int first_channel(int t) { return SPREAD ? (t & ~31) * kGroup + (t & 31) : t * kGroup; }
+template <bool SPREAD> __device__ __forceinline__ int step_of(int i) { return SPREAD ? 32 * i : i; }
+
 // raw words of 16 elements, so that a load can be in flight while earlier values are worked on
 template <class T> struct Raw16 { uint32_t w[16 * sizeof(T) / 4]; };
+__device__ __forceinline__ uint32_t bits_of(const float *p) { return __float_as_uint(*p); }
+__device__ __forceinline__ uint32_t bits_of(const bf16 *p) { return *reinterpret_cast<const uint16_t *>(p); }
 
-// elements p[0 .. n), n <= 16 (n <= 0: none), zeros behind them
-template <class T> __device__ __forceinline__ void load_raw(const T *p, int n, int level, Raw16<T> &r) {
+// elements of p (the thread's first channel), zeros where there is none
+template <bool SPREAD, class T> __device__ __forceinline__ void load_raw(const T *p, int left, Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
-    if (n >= 16 && level == 2) {
+    if constexpr (!SPREAD) {
 #pragma unroll
         for (int i = 0; i < W; i += 8) {
-            uint32_t t[8];
-            ld8(reinterpret_cast<const char *>(p) + 4 * i, t, true);
+            uint32_t t[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            if (left > 0) ld8(reinterpret_cast<const char *>(p) + 4 * i, t, true);
 #pragma unroll
             for (int j = 0; j < 8; j++) r.w[i + j] = t[j];
-        }
-    } else if (n >= 16 && level == 1) {
-#pragma unroll
-        for (int i = 0; i < W; i += 4) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
-            r.w[i] = q.x; r.w[i + 1] = q.y; r.w[i + 2] = q.z; r.w[i + 3] = q.w;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < W; i++) {
-            if constexpr (sizeof(T) == 4) {
-                r.w[i] = i < n ? __float_as_uint(to_f(p[i])) : 0u;
-            } else {
-                const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
-                const uint32_t lo = 2 * i < n ? s[2 * i] : 0u, hi = 2 * i + 1 < n ? s[2 * i + 1] : 0u;
-                r.w[i] = lo | hi << 16;
-            }
+            if constexpr (sizeof(T) == 4) r.w[i] = 32 * i < left ? bits_of(p + 32 * i) : 0u;
+            else r.w[i] = (64 * i < left ? bits_of(p + 64 * i) : 0u) | (64 * i + 32 < left ? bits_of(p + 64 * i + 32) : 0u) << 16;
         }
     }
 }
@@ -109,42 +99,64 @@ __device__ __forceinline__ void pack(const float (&v)[16], Raw16<bf16> &r) {
 #pragma unroll
     for (int i = 0; i < 8; i++) r.w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
 }
-template <class T> __device__ __forceinline__ void store_raw(T *p, int n, int level, const Raw16<T> &r) {
+__device__ __forceinline__ void put_bits(float *p, uint32_t w) { *p = __uint_as_float(w); }
+__device__ __forceinline__ void put_bits(bf16 *p, uint32_t w) { *reinterpret_cast<uint16_t *>(p) = (uint16_t)w; }
+template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, int left, const Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
-    if (n >= 16 && level == 2) {
+    if constexpr (!SPREAD) {
+        if (left > 0) {
 #pragma unroll
-        for (int i = 0; i < W; i += 8) {
-            uint32_t t[8];
+            for (int i = 0; i < W; i += 8) {
+                uint32_t t[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) t[j] = r.w[i + j];
-            st8(reinterpret_cast<char *>(p) + 4 * i, t, true);
-        }
-    } else if (n >= 16 && level == 1) {
-#pragma unroll
-        for (int i = 0; i < W; i += 4)
-            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p) + 4 * i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; i++) {
-            if constexpr (sizeof(T) == 4) {
-                if (i < n) reinterpret_cast<uint32_t *>(p)[i] = r.w[i];
-            } else {
-                uint16_t *s = reinterpret_cast<uint16_t *>(p);
-                if (2 * i < n) s[2 * i] = (uint16_t)r.w[i];
-                if (2 * i + 1 < n) s[2 * i + 1] = (uint16_t)(r.w[i] >> 16);
+                for (int j = 0; j < 8; j++) t[j] = r.w[i + j];
+                st8(reinterpret_cast<char *>(p) + 4 * i, t, true);
             }
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            if (32 * i < left) put_bits(p + 32 * i, sizeof(T) == 4 ? r.w[i * sizeof(T) / 4] : r.w[i / 2] >> (16 * (i & 1)));
     }
 }
-template <class T> __device__ __forceinline__ void load16(const T *p, int n, int level, float (&v)[16]) {
+template <bool SPREAD, class T> __device__ __forceinline__ void load16(const T *p, int left, float (&v)[16]) {
     Raw16<T> r;
-    load_raw(p, n, level, r);
+    load_raw<SPREAD>(p, left, r);
     unpack(r, v);
 }
-template <class T> __device__ __forceinline__ void store16(T *p, int n, int level, const float (&v)[16]) {
+template <bool SPREAD, class T> __device__ __forceinline__ void store16(T *p, int left, const float (&v)[16]) {
     Raw16<T> r;
     pack(v, r);
-    store_raw(p, n, level, r);
+    store_raw<SPREAD>(p, left, r);
+}
+
+// ---------------------------------------------------------------- rows on their way
+// Channels of the rows to come, fetched into shared memory by asynchronous copies of 16 bytes: unlike loads into registers they cost none
+// while they are in flight.  The lanes of a warp that share a row (`lanes` of them, 16 channels each) copy side by side, whole lines per
+// instruction, and wait for each other (__syncwarp behind the wait) before a thread reads its own 16 channels.  A thread's chunks are
+// neighbours, so eight lanes that read their k-th chunk would meet in half or a quarter of the banks: chunk c lies at c ^ (bits 3.. of c).
+// Not for SPREAD.
+__device__ __forceinline__ void copy16(void *dst, const void *src, bool in) {        // in = false: zeros, nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+template <class T> constexpr int kChunks = 16 * (int)sizeof(T) / 16;
+template <class T> __device__ __forceinline__ int chunk_place(int c) { return c ^ ((c >> 3) & (kChunks<T> - 1)); }
+// p: the first of the lanes' channels, `left` of them in the row (a multiple of 32); to: the lanes' part of a stage
+template <class T> __device__ __forceinline__ void fetch_row(uint4 *to, int lanes, int lane, const T *p, int left) {
+#pragma unroll
+    for (int k = 0; k < kChunks<T>; k++) {
+        const int c = k * lanes + lane;
+        copy16(to + chunk_place<T>(c), reinterpret_cast<const char *>(p) + 16 * c, c * (16 / (int)sizeof(T)) < left);
+    }
+}
+template <class T> __device__ __forceinline__ void fetched(const uint4 *from, int lane, Raw16<T> &r) {
+#pragma unroll
+    for (int k = 0; k < kChunks<T>; k++) {
+        const uint4 q = from[chunk_place<T>(lane * kChunks<T> + k)];
+        r.w[4 * k] = q.x; r.w[4 * k + 1] = q.y; r.w[4 * k + 2] = q.z; r.w[4 * k + 3] = q.w;
+    }
 }
 
 // ---------------------------------------------------------------- codes
@@ -158,11 +170,17 @@ template <int CODE> __device__ __forceinline__ uint32_t scale_byte(uint32_t top)
     const int e = (int)(top >> 23) - (CODE == REVNET_INT8 ? 6 : 8) + (m > (CODE == REVNET_INT8 ? 0x7e0000u : 0x600000u) ? 1 : 0);
     return (uint32_t)(e < 10 ? 10 : e);
 }
+// the largest magnitude of 16 values, a NaN if one of them is
+__device__ __forceinline__ float abs_max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
 __device__ __forceinline__ uint32_t abs_max16(const float (&v)[16]) {
-    uint32_t t = 0;
+    float t = abs_max3(v[0], v[1], v[2]);
 #pragma unroll
-    for (int i = 0; i < 16; i++) t = max(t, __float_as_uint(v[i]) & 0x7fffffffu);
-    return t;
+    for (int i = 3; i < 15; i += 2) t = abs_max3(t, v[i], v[i + 1]);
+    return __float_as_uint(abs_max3(t, v[15], v[15])) & 0x7fffffffu;
 }
 // codes of 16 values: the multiplication by a power of two is exact, the one rounding is to nearest even
 template <int CODE> __device__ __forceinline__ uint4 encode16(const float (&v)[16], uint32_t byte) {
@@ -208,19 +226,69 @@ template <int CODE> __device__ __forceinline__ void decode16(uint4 q, uint32_t b
 __device__ __forceinline__ size_t scale_index(const Checkpoint &ck, size_t row, int ch) {
     return ((size_t)(ch >> 7) * ck.rows_pad + row) * 4 + ((ch >> 5) & 3);
 }
-// 16 channels into a checkpoint, by both lanes of a pair at once (all lanes of the warp call it; live: the group lies inside the
-// padded row); v holds zeros behind the row's last channel
-template <int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16]) {
-    uint32_t top = abs_max16(v);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const uint32_t byte = scale_byte<CODE>(top);
-    if (!live) return;
-    *reinterpret_cast<uint4 *>(ck.codes + row * ck.pitch + ch) = encode16<CODE>(v, byte);
-    if ((ch & 16) == 0) ck.scales[scale_index(ck, row, ch)] = (uint8_t)byte;
+// 16 channels into a checkpoint (all lanes of the warp call it, SPREAD: all of one row).  live: the row exists.  v holds zeros behind the row's
+// last channel.  end: first channel that is not to be written (a multiple of 32; 0: the padded row's end).
+template <bool SPREAD, int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16], int end = 0) {
+    if (end == 0) end = ck.pitch;
+    if constexpr (SPREAD) {
+        // the lanes of a warp hold the 32 channels of a block
+        const int ch0 = ch & ~31;
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            if (ch0 + 32 * i >= end) break;
+            const uint32_t byte = scale_byte<CODE>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
+            if (!live) continue;
+            const float inv = __uint_as_float((254u - byte) << 23);
+            uint32_t c;
+            if constexpr (CODE == REVNET_INT8) c = __float_as_uint(__fmaf_rn(v[i], inv, 12582912.f));
+            else c = __nv_cvt_float_to_fp8(v[i] * inv, __NV_SATFINITE, __NV_E4M3);
+            ck.codes[row * ck.pitch + ch + 32 * i] = byte == 255u ? (uint8_t)0 : (uint8_t)c;
+            if ((ch & 31) == 0) ck.scales[scale_index(ck, row, ch + 32 * i)] = (uint8_t)byte;
+        }
+    } else {
+        uint32_t top = abs_max16(v);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        const uint32_t byte = scale_byte<CODE>(top);
+        if (!live || ch >= end) return;
+        *reinterpret_cast<uint4 *>(ck.codes + row * ck.pitch + ch) = encode16<CODE>(v, byte);
+        if ((ch & 16) == 0) ck.scales[scale_index(ck, row, ch)] = (uint8_t)byte;
+    }
 }
-// 16 channels from a checkpoint, ch a multiple of 16
-template <int CODE> __device__ __forceinline__ void read16(const Checkpoint &ck, size_t row, int ch, float (&v)[16]) {
-    const uint4 q = *reinterpret_cast<const uint4 *>(ck.codes + row * ck.pitch + ch);
-    decode16<CODE>(q, byte_of(ck.scales + scale_index(ck, row, ch)), v);
+// 16 channels' codes, not yet decoded: 16 bytes and a scale byte, or (SPREAD) 16 bytes of 16 blocks and their scales
+template <bool SPREAD> struct RawCodes;
+template <> struct RawCodes<false> { uint4 q; uint32_t byte; };
+template <> struct RawCodes<true> { uint4 q, bytes; };
+// left as for load_raw; ch a multiple of 16 unless SPREAD
+template <bool SPREAD> __device__ __forceinline__ void load_codes(const Checkpoint &ck, size_t row, int ch, int left, RawCodes<SPREAD> &r) {
+    if constexpr (SPREAD) {
+        uint32_t c[4] = {0u, 0u, 0u, 0u}, b[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            if (32 * i < left) {
+                c[i / 4] |= byte_of(ck.codes + row * ck.pitch + ch + 32 * i) << (8 * (i & 3));
+                b[i / 4] |= byte_of(ck.scales + scale_index(ck, row, ch + 32 * i)) << (8 * (i & 3));
+            }
+        r.q = make_uint4(c[0], c[1], c[2], c[3]);
+        r.bytes = make_uint4(b[0], b[1], b[2], b[3]);
+    } else if (left > 0) {
+        r.q = *reinterpret_cast<const uint4 *>(ck.codes + row * ck.pitch + ch);
+        r.byte = byte_of(ck.scales + scale_index(ck, row, ch));
+    } else {
+        r.q = make_uint4(0u, 0u, 0u, 0u);
+        r.byte = 0u;
+    }
+}
+template <bool SPREAD, int CODE> __device__ __forceinline__ void decode(const RawCodes<SPREAD> &r, float (&v)[16]) {
+    if constexpr (SPREAD) {
+        decode16<CODE>(r.q, 127u, v);
+        const uint32_t b[4] = {r.bytes.x, r.bytes.y, r.bytes.z, r.bytes.w};
+#pragma unroll
+        for (int i = 0; i < 16; i++) v[i] *= __uint_as_float(((b[i / 4] >> (8 * (i & 3))) & 0xffu) << 23);
+    } else decode16<CODE>(r.q, r.byte, v);
+}
+template <bool SPREAD, int CODE> __device__ __forceinline__ void read16(const Checkpoint &ck, size_t row, int ch, int left, float (&v)[16]) {
+    RawCodes<SPREAD> r;
+    load_codes<SPREAD>(ck, row, ch, left, r);
+    decode<SPREAD, CODE>(r, v);
 }
 #endif

@@ -389,7 +389,7 @@ template <int LANES, int QUADS> void sum_t(Exec &ex, const Wgrad8Args &a) {
 
 // dy for the loads: rows of `pitch` bf16 on 16-byte boundaries.  float32 becomes three parts, the bits of a value 8 at a time: their sum is the
 // value (infinities and NaN stay in the first).  Rows of the last step behind the last one are zeros between the parts.
-template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(const T *dy, int64_t ld, int level, bf16 *out, int rows, int rows_step, int cout, int pitch, FastDiv groups) {
+template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(const T *dy, int64_t ld, bool aligned, bf16 *out, int rows, int rows_step, int cout, int pitch, FastDiv groups) {
     pdl_enter();
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     uint32_t row, g;
@@ -399,7 +399,7 @@ template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(
     const T *src = dy + (size_t)row * ld + ch;
     float v[8];
     if constexpr (sizeof(T) == 4) {
-        if (n == 8 && level >= 1) {
+        if (n == 8 && aligned) {
             const float4 a = reinterpret_cast<const float4 *>(src)[0], b = reinterpret_cast<const float4 *>(src)[1];
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
@@ -490,7 +490,7 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     Wgrad8Args a{};
     a.scales = c.scales; a.gamma = gamma; a.dW = dW; a.partial = (float *)(workspace + w.prepared_bytes); a.status = ex.ctx->dev_status;
     a.rows = (int)d.rows; a.cin = d.cin; a.cout = d.cout; a.row_steps = w.row_steps; a.steps = w.steps; a.tiles_c = w.tiles_c;
-    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = access_level(dW, d.cin, 4);
+    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = rows_aligned(dW, d.cin, 4) ? 2 : (d.cin % 4 == 0 ? 1 : 0);       // (dW itself is on 16 bytes)
     for (int q = 0; q <= w.sharers; q++) a.begin[q] = w.sharers ? (int)((int64_t)w.rest * w.steps * q / w.sharers) : 0;
     for (int t = 0, q = 0; t < w.rest; t++) {
         while (a.begin[q + 1] <= t * w.steps) q++;
@@ -504,9 +504,9 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
         const unsigned grid = (unsigned)(((uint64_t)rows_step * groups + 255) / 256);
         const double bytes = (double)d.rows * d.cout * (d.dy_dtype == REVNET_F32 ? 10 : 4);
         if (d.dy_dtype == REVNET_F32)
-            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<float>, grid, 256, 0, (const float *)dy, d.ld_dy, access_level(dy, d.ld_dy, 4), (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
+            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<float>, grid, 256, 0, (const float *)dy, d.ld_dy, rows_aligned(dy, d.ld_dy, 4), (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
         else
-            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<bf16>, grid, 256, 0, (const bf16 *)dy, d.ld_dy, 0, (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
+            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<bf16>, grid, 256, 0, (const bf16 *)dy, d.ld_dy, false, (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
         ex.check("wgrad8_prepare", bytes);
     }
     void *enc = tc_encoder(ex.ctx);
