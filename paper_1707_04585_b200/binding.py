@@ -103,6 +103,19 @@ def lib():
         for name in EXPORTS:
             if name != "revnet_last_error":
                 getattr(_lib, name).restype = C.c_int
+        # the calls on rows of tokens are short: addresses go through as integers
+        d, p, n = {k: C.POINTER(v) for k, v in (("act", ActDesc), ("norm", NormDesc), ("wgrad", WgradDesc), ("logprob", LogprobDesc))}, C.c_void_p, C.c_size_t
+        _lib.revnet_act_ckpt_bytes.argtypes = [p, C.c_int64, C.c_int, p]
+        _lib.revnet_act_store.argtypes = [p, d["act"]] + [p] * 4
+        _lib.revnet_act_load.argtypes = [p, d["act"]] + [p] * 3
+        _lib.revnet_act_bwd.argtypes = [p, d["act"]] + [p] * 5
+        _lib.revnet_rmsnorm_fwd.argtypes = [p, d["norm"]] + [p] * 8
+        _lib.revnet_rmsnorm_workspace_bytes.argtypes = [p, d["norm"], p]
+        _lib.revnet_rmsnorm_bwd.argtypes = [p, d["norm"]] + [p] * 10 + [n, p]
+        _lib.revnet_linear_wgrad_workspace_bytes.argtypes = [p, d["wgrad"], p]
+        _lib.revnet_linear_wgrad.argtypes = [p, d["wgrad"]] + [p] * 5 + [n, p]
+        _lib.revnet_logprobs_fwd.argtypes = [p, d["logprob"]] + [p] * 8
+        _lib.revnet_logprobs_bwd.argtypes = [p, d["logprob"]] + [p] * 8
     return _lib
 
 
@@ -402,7 +415,6 @@ def revnet_block_fwd_noalloc(ctx, desc, x1, x2, F, G, y1, y2):
 DTYPE = {"f32": 0, "bf16": 1}
 CODE = {"int8": 0, "e4m3": 1}
 ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
-_TYPE_NAMES = ("torch.float32", "torch.bfloat16")
 
 
 def act_desc(rows, channels, dtype="bf16", code="int8", act="none", ld_x=0, ld_a=0) -> ActDesc:
@@ -427,48 +439,76 @@ def _bad(what, name, why):
     raise e
 
 
+_types = None           # torch's types by revnet_dtype, then those of flat buffers; filled at the first call, so that importing this module needs no torch
+F32, BF16, I32, U8 = 0, 1, 2, 3
+
+
+def _type(i):
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
+    return _types[i]
+
+
+def _strided(stride, rows, channels, ld):
+    return (stride[1] == 1 or channels <= 1) and (stride[0] == ld or rows <= 1)
+
+
 def _row_ptr(ctx, what, name, t, rows, channels, ld, dtype):
     """Address of a [rows][channels] tensor (None: null)."""
     if t is None:
         return None
-    if str(t.dtype) != _TYPE_NAMES[dtype] or t.device.type != "cuda" or t.device.index != ctx.device:
-        _bad(what, name, f"must be {_TYPE_NAMES[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
-    if tuple(t.shape) != (rows, channels) or (channels > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or channels)):
+    if t.dtype is not _type(dtype) or t.get_device() != ctx.device or ctx.device < 0:
+        _bad(what, name, f"must be {_type(dtype)} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if t.shape != (rows, channels) or not ((ld or channels) == channels and t.is_contiguous() or _strided(t.stride(), rows, channels, ld or channels)):
         _bad(what, name, f"must be [{rows}][{channels}] with rows {ld or channels} elements apart, got shape {tuple(t.shape)}, strides {t.stride()}")
     return t.data_ptr()
 
 
-def _flat_ptr(ctx, what, name, t, n, dtype="torch.float32"):
+def _flat_ptr(ctx, what, name, t, n, dtype=F32):
     """Address of n contiguous elements, or of at least n bytes (None: null)."""
     if t is None:
         return None
-    if str(t.dtype) != dtype or t.device.type != "cuda" or t.device.index != ctx.device or not t.is_contiguous():
-        _bad(what, name, f"must be contiguous {dtype} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
-    if t.numel() < n if dtype == "torch.uint8" else t.numel() != n:
+    if t.dtype is not _type(dtype) or t.get_device() != ctx.device or ctx.device < 0 or not t.is_contiguous():
+        _bad(what, name, f"must be contiguous {_type(dtype)} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if t.numel() < n if dtype == U8 else t.numel() != n:
         _bad(what, name, f"must hold {n} elements, got {t.numel()}")
     return t.data_ptr()
 
 
 def _ck_bytes(rows, channels):
-    pitch = (channels + 31) // 32 * 32
-    return (rows * pitch + 255) // 256 * 256 + (channels + 127) // 128 * ((rows + 63) // 64 * 64) * 4
+    return (rows * ((channels + 31) & -32) + 255 & -256) + ((channels + 127) >> 7) * ((rows + 63) & -64) * 4
 
 
 def _ck_ptr(ctx, what, name, t, rows, channels):
-    return _flat_ptr(ctx, what, name, t, _ck_bytes(rows, channels), "torch.uint8")
+    return None if t is None else _flat_ptr(ctx, what, name, t, _ck_bytes(rows, channels), U8)
+
+
+def _ws(ctx, what, t):
+    """Address and size of a workspace (None: null, 0)."""
+    if t is None:
+        return None, 0
+    if t.get_device() != ctx.device or not t.is_contiguous():
+        _bad(what, "workspace", f"must be contiguous on cuda:{ctx.device}, got one on {t.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+_raw_stream = None
 
 
 def _stream_of(ctx):
-    import torch
-    return torch.cuda.current_stream(ctx.device).cuda_stream
-
-
-_P = C.c_void_p
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        # (the Stream object that torch.cuda.current_stream makes costs a microsecond and a half)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(ctx.device)
 
 
 def revnet_act_ckpt_bytes(ctx, rows, channels) -> int:
     n = C.c_size_t()
-    ctx.check(lib().revnet_act_ckpt_bytes(ctx.h, C.c_int64(rows), C.c_int(channels), C.byref(n)), "revnet_act_ckpt_bytes")
+    ctx.check(lib().revnet_act_ckpt_bytes(ctx.h, rows, channels, C.byref(n)), "revnet_act_ckpt_bytes")
     return n.value
 
 
@@ -477,87 +517,70 @@ def _a_channels(desc):
 
 
 def revnet_act_store(ctx, desc, x, ck, a=None):
-    w = "revnet_act_store"
-    px = _row_ptr(ctx, w, "x", x, desc.rows, desc.channels, desc.ld_x, desc.dtype)
-    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
-    pa = _row_ptr(ctx, w, "a", a, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
-    ctx.check(lib().revnet_act_store(ctx.h, C.byref(desc), _P(px), _P(pc), _P(pa), _P(_stream_of(ctx))), w)
+    w, rows, c = "revnet_act_store", desc.rows, desc.channels
+    ctx.check(lib().revnet_act_store(ctx.h, desc, _row_ptr(ctx, w, "x", x, rows, c, desc.ld_x, desc.dtype), _ck_ptr(ctx, w, "ck", ck, rows, c),
+                                     _row_ptr(ctx, w, "a", a, rows, _a_channels(desc), desc.ld_a, desc.dtype), _stream_of(ctx)), w)
 
 
 def revnet_act_load(ctx, desc, ck, a):
-    w = "revnet_act_load"
-    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
-    pa = _row_ptr(ctx, w, "a", a, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
-    ctx.check(lib().revnet_act_load(ctx.h, C.byref(desc), _P(pc), _P(pa), _P(_stream_of(ctx))), w)
+    w, rows = "revnet_act_load", desc.rows
+    ctx.check(lib().revnet_act_load(ctx.h, desc, _ck_ptr(ctx, w, "ck", ck, rows, desc.channels),
+                                    _row_ptr(ctx, w, "a", a, rows, _a_channels(desc), desc.ld_a, desc.dtype), _stream_of(ctx)), w)
 
 
 def revnet_act_bwd(ctx, desc, ck, da, dx, a_ck=None):
-    w = "revnet_act_bwd"
-    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.channels)
-    pda = _row_ptr(ctx, w, "da", da, desc.rows, _a_channels(desc), desc.ld_a, desc.dtype)
-    pdx = _row_ptr(ctx, w, "dx", dx, desc.rows, desc.channels, desc.ld_x, desc.dtype)
-    pac = _ck_ptr(ctx, w, "a_ck", a_ck, desc.rows, _a_channels(desc))
-    ctx.check(lib().revnet_act_bwd(ctx.h, C.byref(desc), _P(pc), _P(pda), _P(pdx), _P(pac), _P(_stream_of(ctx))), w)
-
-
-def _norm_ptrs(ctx, w, d, stream, branch, channels, ck):
-    out = {n: _row_ptr(ctx, w, n, t, d.rows, d.channels, d.ld_stream, d.stream_dtype) for n, t in stream}
-    out.update((n, _row_ptr(ctx, w, n, t, d.rows, d.channels, d.ld_branch, d.branch_dtype)) for n, t in branch)
-    out.update((n, _flat_ptr(ctx, w, n, t, d.rows if n == "rstd" else d.channels)) for n, t in channels)
-    out["ck"] = _ck_ptr(ctx, w, "ck", ck, d.rows, d.channels)
-    return {n: _P(p) for n, p in out.items()}
+    w, rows, c, ca = "revnet_act_bwd", desc.rows, desc.channels, _a_channels(desc)
+    ctx.check(lib().revnet_act_bwd(ctx.h, desc, _ck_ptr(ctx, w, "ck", ck, rows, c), _row_ptr(ctx, w, "da", da, rows, ca, desc.ld_a, desc.dtype),
+                                   _row_ptr(ctx, w, "dx", dx, rows, c, desc.ld_x, desc.dtype), _ck_ptr(ctx, w, "a_ck", a_ck, rows, ca), _stream_of(ctx)), w)
 
 
 def revnet_rmsnorm_fwd(ctx, desc, x, r, gamma, h, n, ck, rstd):
-    w = "revnet_rmsnorm_fwd"
-    p = _norm_ptrs(ctx, w, desc, (("x", x), ("h", h)), (("r", r), ("n", n)), (("gamma", gamma), ("rstd", rstd)), ck)
-    ctx.check(lib().revnet_rmsnorm_fwd(ctx.h, C.byref(desc), p["x"], p["r"], p["gamma"], p["h"], p["n"], p["ck"], p["rstd"], _P(_stream_of(ctx))), w)
+    w, rows, c, ls, lb, ts, tb = "revnet_rmsnorm_fwd", desc.rows, desc.channels, desc.ld_stream, desc.ld_branch, desc.stream_dtype, desc.branch_dtype
+    ctx.check(lib().revnet_rmsnorm_fwd(
+        ctx.h, desc, _row_ptr(ctx, w, "x", x, rows, c, ls, ts), _row_ptr(ctx, w, "r", r, rows, c, lb, tb), _flat_ptr(ctx, w, "gamma", gamma, c),
+        _row_ptr(ctx, w, "h", h, rows, c, ls, ts), _row_ptr(ctx, w, "n", n, rows, c, lb, tb), _ck_ptr(ctx, w, "ck", ck, rows, c),
+        _flat_ptr(ctx, w, "rstd", rstd, rows), _stream_of(ctx)), w)
 
 
 def revnet_rmsnorm_workspace_bytes(ctx, desc) -> int:
     n = C.c_size_t()
-    ctx.check(lib().revnet_rmsnorm_workspace_bytes(ctx.h, C.byref(desc), C.byref(n)), "revnet_rmsnorm_workspace_bytes")
+    ctx.check(lib().revnet_rmsnorm_workspace_bytes(ctx.h, desc, C.byref(n)), "revnet_rmsnorm_workspace_bytes")
     return n.value
 
 
 def revnet_rmsnorm_bwd(ctx, desc, dn, dh, h, ck, rstd, gamma, dx, dr, dgamma, workspace):
-    w = "revnet_rmsnorm_bwd"
-    p = _norm_ptrs(ctx, w, desc, (("dh", dh), ("h", h), ("dx", dx)), (("dn", dn), ("dr", dr)), (("rstd", rstd), ("gamma", gamma), ("dgamma", dgamma)), ck)
-    size = C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size())
-    ctx.check(lib().revnet_rmsnorm_bwd(ctx.h, C.byref(desc), p["dn"], p["dh"], p["h"], p["ck"], p["rstd"], p["gamma"], p["dx"], p["dr"], p["dgamma"],
-                                       _ptr(workspace), size, _P(_stream_of(ctx))), w)
+    w, rows, c, ls, lb, ts, tb = "revnet_rmsnorm_bwd", desc.rows, desc.channels, desc.ld_stream, desc.ld_branch, desc.stream_dtype, desc.branch_dtype
+    ws, size = _ws(ctx, w, workspace)
+    ctx.check(lib().revnet_rmsnorm_bwd(
+        ctx.h, desc, _row_ptr(ctx, w, "dn", dn, rows, c, lb, tb), _row_ptr(ctx, w, "dh", dh, rows, c, ls, ts), _row_ptr(ctx, w, "h", h, rows, c, ls, ts),
+        _ck_ptr(ctx, w, "ck", ck, rows, c), _flat_ptr(ctx, w, "rstd", rstd, rows), _flat_ptr(ctx, w, "gamma", gamma, c),
+        _row_ptr(ctx, w, "dx", dx, rows, c, ls, ts), _row_ptr(ctx, w, "dr", dr, rows, c, lb, tb), _flat_ptr(ctx, w, "dgamma", dgamma, c), ws, size, _stream_of(ctx)), w)
 
 
 def revnet_linear_wgrad_workspace_bytes(ctx, desc) -> int:
     n = C.c_size_t()
-    ctx.check(lib().revnet_linear_wgrad_workspace_bytes(ctx.h, C.byref(desc), C.byref(n)), "revnet_linear_wgrad_workspace_bytes")
+    ctx.check(lib().revnet_linear_wgrad_workspace_bytes(ctx.h, desc, C.byref(n)), "revnet_linear_wgrad_workspace_bytes")
     return n.value
 
 
 def revnet_linear_wgrad(ctx, desc, dy, ck, gamma, dW, workspace):
-    w = "revnet_linear_wgrad"
-    pdy = _row_ptr(ctx, w, "dy", dy, desc.rows, desc.cout, desc.ld_dy, desc.dy_dtype)
-    pc = _ck_ptr(ctx, w, "ck", ck, desc.rows, desc.cin)
-    pg = _flat_ptr(ctx, w, "gamma", gamma, desc.cin)
-    pw = _flat_ptr(ctx, w, "dW", dW, desc.cin * desc.cout)
-    size = C.c_size_t(0 if workspace is None else workspace.numel() * workspace.element_size())
-    ctx.check(lib().revnet_linear_wgrad(ctx.h, C.byref(desc), _P(pdy), _P(pc), _P(pg), _P(pw), _ptr(workspace), size, _P(_stream_of(ctx))), w)
+    w, rows, ci, co = "revnet_linear_wgrad", desc.rows, desc.cin, desc.cout
+    ws, size = _ws(ctx, w, workspace)
+    ctx.check(lib().revnet_linear_wgrad(ctx.h, desc, _row_ptr(ctx, w, "dy", dy, rows, co, desc.ld_dy, desc.dy_dtype), _ck_ptr(ctx, w, "ck", ck, rows, ci),
+                                        _flat_ptr(ctx, w, "gamma", gamma, ci), _flat_ptr(ctx, w, "dW", dW, ci * co), ws, size, _stream_of(ctx)), w)
 
 
 def revnet_logprobs_fwd(ctx, desc, logits, targets, logp, entropy, lse, top_logp=None, top_index=None):
-    w = "revnet_logprobs_fwd"
-    px = _row_ptr(ctx, w, "logits", logits, desc.rows, desc.vocab, desc.ld, desc.dtype)
-    pt = _flat_ptr(ctx, w, "targets", targets, desc.rows, "torch.int32")
-    rows = [_P(_flat_ptr(ctx, w, n, t, desc.rows)) for n, t in (("logp", logp), ("entropy", entropy), ("lse", lse))]
-    pl = _flat_ptr(ctx, w, "top_logp", top_logp, desc.rows * desc.k)
-    pi = _flat_ptr(ctx, w, "top_index", top_index, desc.rows * desc.k, "torch.int32")
-    ctx.check(lib().revnet_logprobs_fwd(ctx.h, C.byref(desc), _P(px), _P(pt), *rows, _P(pl), _P(pi), _P(_stream_of(ctx))), w)
+    w, rows = "revnet_logprobs_fwd", desc.rows
+    ctx.check(lib().revnet_logprobs_fwd(
+        ctx.h, desc, _row_ptr(ctx, w, "logits", logits, rows, desc.vocab, desc.ld, desc.dtype), _flat_ptr(ctx, w, "targets", targets, rows, I32),
+        _flat_ptr(ctx, w, "logp", logp, rows), _flat_ptr(ctx, w, "entropy", entropy, rows), _flat_ptr(ctx, w, "lse", lse, rows),
+        _flat_ptr(ctx, w, "top_logp", top_logp, rows * desc.k), _flat_ptr(ctx, w, "top_index", top_index, rows * desc.k, I32), _stream_of(ctx)), w)
 
 
 def revnet_logprobs_bwd(ctx, desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits):
-    w = "revnet_logprobs_bwd"
-    px = _row_ptr(ctx, w, "logits", logits, desc.rows, desc.vocab, desc.ld, desc.dtype)
-    pd = _row_ptr(ctx, w, "dlogits", dlogits, desc.rows, desc.vocab, desc.ld, desc.dtype)
-    pt = _flat_ptr(ctx, w, "targets", targets, desc.rows, "torch.int32")
-    rows = [_P(_flat_ptr(ctx, w, n, t, desc.rows)) for n, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy))]
-    ctx.check(lib().revnet_logprobs_bwd(ctx.h, C.byref(desc), _P(px), _P(pt), *rows, _P(pd), _P(_stream_of(ctx))), w)
+    w, rows = "revnet_logprobs_bwd", desc.rows
+    ctx.check(lib().revnet_logprobs_bwd(
+        ctx.h, desc, _row_ptr(ctx, w, "logits", logits, rows, desc.vocab, desc.ld, desc.dtype), _flat_ptr(ctx, w, "targets", targets, rows, I32),
+        _flat_ptr(ctx, w, "lse", lse, rows), _flat_ptr(ctx, w, "entropy", entropy, rows), _flat_ptr(ctx, w, "dlogp", dlogp, rows),
+        _flat_ptr(ctx, w, "dentropy", dentropy, rows), _row_ptr(ctx, w, "dlogits", dlogits, rows, desc.vocab, desc.ld, desc.dtype), _stream_of(ctx)), w)

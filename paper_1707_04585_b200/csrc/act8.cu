@@ -13,7 +13,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // act(x) and d act / dx.  1 / (1 + e^-x): e^-x = inf gives 0, which is right to float32's least normal number.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return rcp_ftz(1.f + exp2_ftz(-1.4426950408889634f * x)); }
 __device__ __forceinline__ float gelu_arg(float x) { return 1.5957691216057308f * (x + 0.044715f * x * x * x); }   // 2 sqrt(2 / pi) (...)
 template <int ACT> __device__ __forceinline__ float act(float x) {
     if (ACT == REVNET_ACT_RELU) return x > 0.f ? x : (x != x ? x : 0.f);

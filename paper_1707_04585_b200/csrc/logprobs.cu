@@ -4,12 +4,13 @@
 //   backward  dx = dlogp (1[target] - p) - dentropy p (log p + entropy),  p = e^(x - lse)
 //
 // HBM bounds both: the logits are read once.  A thread carries the running (m, s, t) of its elements and rescales them when its maximum
-// rises; the threads' triples are joined at the end by the same rule.  With few rows a row is split over the CTAs of a cluster, which
+// rises; the threads' triples are joined at the end by the same rule.  In bf16 the instructions per logit bound it next to HBM (one
+// exponential, a conversion, half a maximum), so sums and products go two at a time (f32x2).  With few rows a row is split over the CTAs of a cluster, which
 // join through distributed shared memory: no workspace, no second launch.
 // The k most likely tokens: every warp keeps a sorted list of its own, one entry per lane, of keys (logit, then the lower index) as 64-bit
 // integers.  A logit is looked at again only if it reaches the largest k-th entry of any list of the CTA, which after the first few hundred
-// is rare in any order but an ascending one (n elements in random order change a list k ln(n / k) times); the first bound is the k-th largest of
-// a warp's 32 lanes' maxima.  Leaving out what no list needs changes no result.
+// is rare in any order but an ascending one (n elements in random order change a list k ln(n / k) times); a list begins as the sorted maxima of
+// the warp's 32 lanes.  Leaving out what no list needs changes no result.  Lists are joined pairwise by a bitonic merge.
 // Rows need not be aligned: elements in front of the first 32-byte boundary and behind the last are read one by one.
 #include "token.cuh"
 #include <math.h>
@@ -33,11 +34,10 @@ struct LogpArgs {
 
 // a row's running sums: m the maximum (in units of log 2: y = x log2 e), s = sum 2^(y - m), t = sum (y - m) 2^(y - m)
 struct Sums { float m, s, t; };
-__device__ __forceinline__ float exp2_fast(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 // a's sums as they are for the maximum m >= a.m; an empty or all -inf one (m = -inf) is zero for any m
 __device__ __forceinline__ void rescale(Sums &a, float m) {
     if (a.m == -INFINITY || a.m == m) { a.m = m; return; }
-    const float d = a.m - m, e = exp2_fast(d);
+    const float d = a.m - m, e = exp2_ftz(d);
     a.t = (a.t + d * a.s) * e;
     a.s *= e;
     if (e == 0.f) a.t = 0.f;         // d = -inf: m is +inf, and the row's sums are NaN through its own element
@@ -49,18 +49,48 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
     rescale(b, m);
     return Sums{m, a.s + b.s, a.t + b.t};
 }
-// N logits, top the largest of them
+// two float32 operations in one instruction
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 two(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ void parts(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float both(f32x2 v) { float lo, hi; parts(v, lo, hi); return lo + hi; }
+
+// N logits, N a multiple of 4 or 1, top the largest of them
 template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N], float top) {
     top *= kLog2e;
     if (top > a.m) rescale(a, top);
     // (a.m stays -inf while every logit so far is: then all differences would be NaN)
     const float m = a.m == -INFINITY ? 0.f : a.m;
+    float s, t;
+    if constexpr (N == 1) {
+        const float d = fmaf(x[0], kLog2e, -m);
+        s = exp2_ftz(d);
+        t = d * s;
+    } else {
+        const f32x2 l = two(kLog2e, kLog2e), mm = two(-m, -m);
+        f32x2 ss[2] = {0ull, 0ull}, tt[2] = {0ull, 0ull};
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        const float d = fmaf(x[i], kLog2e, -m), e = exp2_fast(d);
-        a.s += e;
-        a.t = fmaf(fmaxf(d, -200.f), e, a.t);        // 0 log 0 = 0: e is 0 far before -200 (fmaxf also drops a NaN, which s carries)
+        for (int i = 0; i < N; i += 2) {
+            const f32x2 d = fma2(two(x[i], x[i + 1]), l, mm);
+            float d0, d1;
+            parts(d, d0, d1);
+            const f32x2 e = two(exp2_ftz(d0), exp2_ftz(d1));
+            ss[(i / 2) & 1] = add2(ss[(i / 2) & 1], e);
+            tt[(i / 2) & 1] = fma2(d, e, tt[(i / 2) & 1]);
+        }
+        s = both(add2(ss[0], ss[1]));
+        t = both(add2(tt[0], tt[1]));
     }
+    if (t != t && s == s) {
+        // 0 log 0 = 0: -inf among them (e is 0 far before -200; fmaxf would drop a NaN, but s has none)
+        t = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; i++) { const float d = fmaf(x[i], kLog2e, -m); t = fmaf(fmaxf(d, -200.f), exp2_ftz(d), t); }
+    }
+    a.s += s;
+    a.t += t;
 }
 __device__ __forceinline__ float top_of(const Raw16<float> &r) {
     float t = __uint_as_float(r.w[0]);
@@ -87,36 +117,53 @@ __device__ __forceinline__ float value_of(unsigned long long key) {
     const uint32_t b = (uint32_t)(key >> 32);
     return b == 0xffffffffu ? NAN : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
+typedef unsigned long long Key;
+__device__ __forceinline__ Key larger(Key a, Key b) { return a > b ? a : b; }
+__device__ __forceinline__ Key smaller(Key a, Key b) { return a < b ? a : b; }
+// descending lists of a warp, one key per lane: sort 32 keys; the 32 largest of two lists
+__device__ __forceinline__ Key sorted(Key v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int stride = size / 2; stride; stride /= 2) {
+            const Key o = __shfl_xor_sync(0xffffffffu, v, stride);
+            v = ((lane & stride) == 0) == ((lane & size) == 0) ? larger(v, o) : smaller(v, o);
+        }
+    return v;
+}
+__device__ __forceinline__ Key merged(Key a, Key b) {
+    const int lane = threadIdx.x & 31;
+    Key v = larger(a, __shfl_sync(0xffffffffu, b, 31 - lane));           // one list up, the other down: a bitonic sequence
+#pragma unroll
+    for (int stride = 16; stride; stride /= 2) {
+        const Key o = __shfl_xor_sync(0xffffffffu, v, stride);
+        v = (lane & stride) == 0 ? larger(v, o) : smaller(v, o);
+    }
+    return v;
+}
 struct TopList {                     // lane i: the i-th largest key so far, 0 for none; least: keys up to this one are not needed
-    unsigned long long mine, least;
+    Key mine, least;
     int k;
-    __device__ __forceinline__ void offer(unsigned long long key) {       // one key per lane; the whole warp calls
+    __device__ __forceinline__ void raise() { least = larger(least, __shfl_sync(0xffffffffu, mine, k - 1)); }
+    __device__ __forceinline__ void offer(Key key) {                     // one key per lane; the whole warp calls
         unsigned todo = __ballot_sync(0xffffffffu, key > least);
         const int lane = threadIdx.x & 31;
+        if (__popc(todo) > 6) {      // a sort and a merge are 20 exchanges, an insertion about three
+            mine = merged(mine, sorted(key > least ? key : 0ull));
+            raise();
+            return;
+        }
         while (todo) {
             const int src = __ffs(todo) - 1;
             todo &= todo - 1;
-            const unsigned long long c = __shfl_sync(0xffffffffu, key, src);
+            const Key c = __shfl_sync(0xffffffffu, key, src);
             if (c <= least) continue;
             const int at = __popc(__ballot_sync(0xffffffffu, mine > c));
-            const unsigned long long up = __shfl_up_sync(0xffffffffu, mine, 1);
+            const Key up = __shfl_up_sync(0xffffffffu, mine, 1);
             mine = lane < at ? mine : (lane == at ? c : up);
-            const unsigned long long kth = __shfl_sync(0xffffffffu, mine, k - 1);
-            if (kth > least) least = kth;
+            raise();
         }
-    }
-    // a first bound from one logit per lane (order 0: none): the k-th largest of the 32, below every key of that logit
-    __device__ __forceinline__ void bound(uint32_t order) {
-        const int lane = threadIdx.x & 31;
-        int rank = 0;
-#pragma unroll
-        for (int j = 0; j < 32; j++) {
-            const uint32_t o = __shfl_sync(0xffffffffu, order, j);
-            rank += o > order || (o == order && j < lane) ? 1 : 0;
-        }
-        const unsigned at = __ballot_sync(0xffffffffu, rank == k - 1);
-        const unsigned long long b = (unsigned long long)__shfl_sync(0xffffffffu, order, __ffs(at) - 1) << 32;
-        if (b > least) least = b;
     }
 };
 
@@ -143,9 +190,9 @@ constexpr int kVec = 16;             // logits per step of a thread
 
 // CLUSTER: the row's CTAs are a cluster along x; else one CTA per row
 template <class T, bool TOP, bool CLUSTER>
-__global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
+__global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) {
     __shared__ float sm_m[16], sm_s[16], sm_t[16];
-    __shared__ unsigned long long lists[TOP ? 16 * 32 : 1], best;        // best: the largest k-th key of a warp's list
+    __shared__ Key lists[TOP ? 16 * 32 : 1], best;        // best: the largest k-th key of a warp's list
     pdl_enter();
     const uint32_t rank = CLUSTER ? cluster_rank() : 0, ctas = CLUSTER ? cluster_size() : 1;
     const size_t row = blockIdx.x / ctas;
@@ -166,6 +213,9 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
 
     // whole warps go round the loop: the list's shuffles need all lanes.  The next vector is on its way while one is worked on.
     Raw16<T> raw, next;
+    float bar = -INFINITY;           // the bound as a logit, and the largest index that still reaches it
+    unsigned bar_index = 0xffffffffu;
+    bool started = false;
     if ((int)threadIdx.x < vecs) load_raw<false>(xb + head + (int)threadIdx.x * kVec, kVec, next);
     for (int v0 = warp * 32; v0 < vecs; v0 += blockDim.x) {
         const int v = v0 + lane;
@@ -177,25 +227,35 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
         unpack(raw, f);
         if (ok) add(sum, f, top);
         if constexpr (TOP) {
-            const unsigned long long other = __shfl_sync(0xffffffffu, *(volatile unsigned long long *)&best, 0);
-            if (other > list.least) list.least = other;
+            const int i0 = begin + head + v * kVec;
             const bool nan = sum.s != sum.s;                             // (one of this thread's logits so far)
-            if (list.least == 0ull) list.bound(ok ? (nan ? 1u : order_of(top)) : 0u);
-            bool look = ok && (nan || order_of(top) >= (uint32_t)(list.least >> 32));
-            if (__any_sync(0xffffffffu, look)) {
-                const float bar = list.least ? value_of(list.least) : -INFINITY;
+            if (__any_sync(0xffffffffu, ok && (nan || top > bar || (top == bar && (unsigned)i0 <= bar_index)))) {
+                list.least = larger(list.least, __shfl_sync(0xffffffffu, *(volatile Key *)&best, 0));
+                uint32_t taken = 0;                                      // of this lane's vector: the logit that is in the list already
+                if (!started) {
+                    started = true;
+                    if (ok && !nan) {
+#pragma unroll
+                        for (int i = kVec - 1; i >= 0; i--) taken = f[i] == top ? 1u << i : taken;
+                    }
+                    list.mine = sorted(taken ? key_of(top, i0 + __ffs(taken) - 1) : 0ull);
+                    list.raise();
+                }
+                bar = list.least ? value_of(list.least) : -INFINITY;
                 uint32_t todo = 0;
-                if (look) {
+                if (ok && (nan || top >= bar)) {
 #pragma unroll
                     for (int i = 0; i < kVec; i++) todo |= !(f[i] < bar) ? 1u << i : 0u;
                 }
+                todo &= ~taken;
                 while (__any_sync(0xffffffffu, todo != 0)) {
-                    const int i = begin + head + v * kVec + (todo ? __ffs(todo) - 1 : 0);
+                    const int i = i0 + (todo ? __ffs(todo) - 1 : 0);
                     list.offer(todo ? key_of(to_f(x[i]), i) : 0ull);
                     todo &= todo - 1;
                 }
-                const unsigned long long kth = __shfl_sync(0xffffffffu, list.mine, p.k - 1);
-                if (lane == 0 && kth > other) atomicMax(&best, kth);
+                if (lane == p.k - 1 && list.mine > 0ull) atomicMax(&best, list.mine);
+                bar = list.least ? value_of(list.least) : -INFINITY;
+                bar_index = ~(unsigned)list.least;
             }
         }
     }
@@ -212,19 +272,19 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
         sum = join(sum, b);
     }
     if (lane == 0) { sm_m[warp] = sum.m; sm_s[warp] = sum.s; sm_t[warp] = sum.t; }
-    if constexpr (TOP) lists[warp * 32 + lane] = lane < p.k ? list.mine : 0ull;
+    if constexpr (TOP) lists[warp * 32 + lane] = list.mine;
     __syncthreads();
+    if constexpr (TOP)
+        for (int off = warps / 2; off; off /= 2) {
+            if (warp < off) lists[warp * 32 + lane] = list.mine = merged(list.mine, lists[(warp + off) * 32 + lane]);
+            __syncthreads();
+        }
     if (warp == 0) {
         // lane w: the sums of warp w
         sum = lane < warps ? Sums{sm_m[lane], sm_s[lane], sm_t[lane]} : Sums{-INFINITY, 0.f, 0.f};
         for (int o = 16; o; o >>= 1) {
             const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
             sum = join(sum, b);
-        }
-        if constexpr (TOP) {
-            list.least = __shfl_sync(0xffffffffu, list.mine, p.k - 1);   // (the bound may be a key of another list)
-            for (int w = 1; w < warps; w++) list.offer(lists[w * 32 + lane]);
-            if (CLUSTER) { __syncwarp(); lists[lane] = lane < p.k ? list.mine : 0ull; }
         }
         if (CLUSTER && lane == 0) { sm_m[0] = sum.m; sm_s[0] = sum.s; sm_t[0] = sum.t; }
     }
@@ -236,8 +296,14 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
                 const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
                 sum = join(sum, b);
             }
-            if constexpr (TOP)
-                for (uint32_t c = 1; c < ctas; c++) list.offer(remote(&lists[lane], c));
+            if constexpr (TOP) {
+                Key others[8];
+#pragma unroll
+                for (uint32_t c = 1; c < 8; c++) others[c] = c < ctas ? remote(&lists[lane], c) : 0ull;
+#pragma unroll
+                for (uint32_t c = 1; c < 8; c++)
+                    if (c < ctas) list.mine = merged(list.mine, others[c]);
+            }
         }
         cluster_sync();              // nobody leaves while rank 0 reads
         if (rank != 0) return;
@@ -266,7 +332,7 @@ __global__ void __launch_bounds__(512) logprobs_fwd_kernel(const LogpArgs p) {
 
 // one logit's gradient
 __device__ __forceinline__ float grad(float x, float lse, float g, float ge, float ent2) {
-    const float l = (x - lse) * kLog2e, q = exp2_fast(l);
+    const float l = (x - lse) * kLog2e, q = exp2_ftz(l);
     // ge log p in natural units: ge (l + ent2) ln 2, the factor folded into ge by the caller
     return q == 0.f ? 0.f : -q * fmaf(ge, l + ent2, g);
 }
@@ -334,11 +400,14 @@ void logprobs_fwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, co
     LogpArgs p{};
     p.x = logits; p.targets = targets; p.logp = logp; p.ent = entropy; p.lse = lse; p.top_logp = top_logp; p.top_index = top_index;
     p.rows = d.rows; p.ld = d.ld; p.vocab = d.vocab; p.k = d.k; p.status = ex.ctx->dev_status;
+    // 1024 threads per SM (64 registers each): small CTAs where there are rows for all of them, since every CTA has its own start and end (4096 rows
+    // of 50000: 97 us with 512 threads, 79 with 128); few rows take large CTAs, and more than one where their parts stay longer than one step
+    const int64_t sms = ex.ctx->sm_count;
+    const unsigned most = d.rows <= 2 * sms ? 512 : (d.rows <= 6 * sms ? 256 : 128);
     unsigned threads = 32;
-    while (threads < 512 && (int)threads * kVec < d.vocab) threads *= 2;
-    // a row is split while its parts stay longer than one step of a CTA and the GPU has SMs to spare
+    while (threads < most && (int)threads * kVec < d.vocab) threads *= 2;
     int cluster = 1;
-    while (cluster < 8 && d.rows * cluster * 2 <= 4 * ex.ctx->sm_count && d.vocab / (cluster * 2) >= (int)threads * kVec) cluster *= 2;
+    while (cluster < 8 && d.rows * cluster * 2 * threads <= sms * 1280 && d.vocab / (cluster * 2) >= (int)threads * kVec) cluster *= 2;
     p.chunk = (d.vocab + cluster - 1) / cluster;
     const double bytes = (double)d.rows * d.vocab * (d.dtype == REVNET_F32 ? 4 : 2);
     if (d.dtype == REVNET_F32) fwd_t<float>(ex, p, cluster, threads);

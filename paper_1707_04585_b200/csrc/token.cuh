@@ -38,6 +38,10 @@ void logprobs_bwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, co
                   const float *dlogp, const float *dentropy, void *dlogits);
 
 #ifdef __CUDACC__
+// 2^v to two steps of 2^-23, results below 2^-126 become 0 (keeping those takes four more instructions); 1 / v likewise
+__device__ __forceinline__ float exp2_ftz(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float rcp_ftz(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+
 // ---------------------------------------------------------------- sixteen channels of a row
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }

@@ -135,9 +135,9 @@ def _arg(x, kind):
 
 
 def act_tol(x, kind):
-    """Bounds on the float32 errors of act and of its derivative.  __expf is off by (2 + 1.17 |arg|) steps of 2^-23 and its argument by three
-    roundings, __fdividef by two steps, the sum 1 + e by half of one: (8 + 2 |arg|) steps for the sigmoid s, relative, and as much, absolute, of
-    s for 1 - s; the products add five."""
+    """Bounds on the float32 errors of act and of its derivative.  e^arg as 2^(arg log2 e) is off by 2 steps of 2^-23 and by 1.17 |arg| through the
+    rounded product, arg itself by three roundings, the reciprocal by two steps, the sum 1 + e by half of one: (8 + 2 |arg|) steps for the sigmoid s,
+    relative, and as much, absolute, of s for 1 - s; the products add five."""
     if kind in ("none", "relu"):
         return torch.zeros_like(x), torch.zeros_like(x)
     k = GELU_K * (1 + 3 * 0.044715 * x * x) if kind == "gelu" else torch.ones_like(x)
