@@ -196,6 +196,17 @@ int revnet_transition_bwd(revnet_ctx *ctx, const revnet_transition_desc *desc,
                           float *din1, float *din2, float *dW, float *dgamma, float *dbeta,
                           void *workspace, size_t workspace_bytes, void *stream);
 
+/* The same layer with its input kept in 8 bits (the checkpoint format under "operators on rows of tokens" below, code a revnet_code)
+ * instead of 32: revnet_transition_keep, after the forward call, fills a caller-owned buffer (256-byte aligned) of
+ * revnet_transition_kept_bytes, and the input may go; revnet_transition_bwd_kept is revnet_transition_bwd on the float32 values that the
+ * buffer holds, with the statistics of those values (workspace: revnet_transition_kept_bytes too). */
+int revnet_transition_kept_bytes(revnet_ctx *ctx, const revnet_transition_desc *desc, size_t *kept_bytes, size_t *bwd_workspace_bytes);
+int revnet_transition_keep(revnet_ctx *ctx, const revnet_transition_desc *desc, const void *in1, const void *in2, int code, void *kept, void *stream);
+int revnet_transition_bwd_kept(revnet_ctx *ctx, const revnet_transition_desc *desc, int code, const void *kept,
+                               const float *dout1, const float *dout2, const float *W, const float *gamma, const float *beta,
+                               float *din1, float *din2, float *dW, float *dgamma, float *dbeta,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- classification stack (Section 3.2: only non-reversible layers keep their inputs) ---- */
 
 typedef struct {
@@ -378,7 +389,9 @@ int revnet_rmsnorm_bwd(revnet_ctx *ctx, const revnet_norm_desc *desc, const void
 /* Weight gradient of a linear layer (a 1x1 convolution) whose input was kept in 8 bits:
  *   dW[o][c] = gamma[c] * sum over rows t of dy[t][o] * x8[t][c],   dW [cout][cin] float32, overwritten
  * on the tensor cores.  Products are exact: x8 and a bf16 dy are bf16 operands; a float32 dy is split into three bf16 numbers that
- * together hold all its 24 bits (three products).  gamma null: ones. */
+ * together hold all its 24 bits (three products).  gamma null: ones.  Sums are kept in float32, rounded to nearest at least every 2048
+ * rows.  bf16 rows a multiple of 16 bytes apart are read from where they are and must start on 16 bytes (REVNET_E_MISALIGNED); any other
+ * dy is laid out in the workspace first. */
 typedef struct {
     int64_t rows;            /* < 2^29 */
     int cin, cout;           /* 1 .. 65536 */

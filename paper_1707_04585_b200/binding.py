@@ -25,6 +25,7 @@ EXPORTS = ["revnet_create", "revnet_destroy", "revnet_last_error", "revnet_block
            "revnet_transition_workspace_bytes", "revnet_transition_fwd", "revnet_transition_bwd",
            "revnet_block_fwd_noalloc", "revnet_block_pack_bytes", "revnet_pack_weights", "revnet_selftest_bounded_wait",
            "revnet_plan_set_buffer_sizes",
+           "revnet_transition_kept_bytes", "revnet_transition_keep", "revnet_transition_bwd_kept",
            "revnet_act_ckpt_bytes", "revnet_act_store", "revnet_act_load", "revnet_act_bwd",
            "revnet_rmsnorm_fwd", "revnet_rmsnorm_workspace_bytes", "revnet_rmsnorm_bwd",
            "revnet_linear_wgrad_workspace_bytes", "revnet_linear_wgrad", "revnet_logprobs_fwd", "revnet_logprobs_bwd"]
@@ -399,6 +400,27 @@ def revnet_transition_bwd(ctx, desc, in1, in2, dout1, dout2, W, gamma, beta, din
     ctx.check(lib().revnet_transition_bwd(ctx.h, C.byref(desc), _ptr(in1), _ptr(in2), _ptr(dout1), _ptr(dout2), _ptr(W),
                                           _ptr(gamma), _ptr(beta), _ptr(din1), _ptr(din2), _ptr(dW), _ptr(dgamma), _ptr(dbeta),
                                           _ptr(workspace), _nbytes(workspace), _stream()), "revnet_transition_bwd")
+
+
+def revnet_transition_kept_bytes(ctx, desc):
+    """-> (bytes of the buffer that keeps the layer's input in 8 bits, workspace of the backward call that reads it)"""
+    k, w = C.c_size_t(), C.c_size_t()
+    ctx.check(lib().revnet_transition_kept_bytes(ctx.h, C.byref(desc), C.byref(k), C.byref(w)), "revnet_transition_kept_bytes")
+    return k.value, w.value
+
+
+def revnet_transition_keep(ctx, desc, in1, in2, code, kept):
+    if kept.numel() * kept.element_size() < revnet_transition_kept_bytes(ctx, desc)[0]:
+        _bad("revnet_transition_keep", "kept", "is too small")
+    ctx.check(lib().revnet_transition_keep(ctx.h, C.byref(desc), _ptr(in1), _ptr(in2), C.c_int(CODE[code]), _ptr(kept), _stream()), "revnet_transition_keep")
+
+
+def revnet_transition_bwd_kept(ctx, desc, code, kept, dout1, dout2, W, gamma, beta, din1, din2, dW, dgamma, dbeta, workspace):
+    if kept.numel() * kept.element_size() < revnet_transition_kept_bytes(ctx, desc)[0]:
+        _bad("revnet_transition_bwd_kept", "kept", "is too small")
+    ctx.check(lib().revnet_transition_bwd_kept(ctx.h, C.byref(desc), C.c_int(CODE[code]), _ptr(kept), _ptr(dout1), _ptr(dout2), _ptr(W), _ptr(gamma),
+                                               _ptr(beta), _ptr(din1), _ptr(din2), _ptr(dW), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
+                                               _nbytes(workspace), _stream()), "revnet_transition_bwd_kept")
 
 
 def revnet_block_fwd_noalloc(ctx, desc, x1, x2, F, G, y1, y2):

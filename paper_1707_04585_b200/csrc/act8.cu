@@ -41,11 +41,12 @@ struct Act8Args {
     int64_t ld_x, ld_a;              // of x, a above
     uint32_t total;                  // groups (SPREAD: warps' 512 channels) in all
     FastDiv per_row;                 // of a row
+    float q;                         // not 0: x is int32 fixed point, value = i * q (a coupling state)
 };
 
 // this thread's row and first channel; false behind the last row
 template <bool SPREAD> __device__ __forceinline__ bool place(const Act8Args &p, size_t &row, int &ch) {
-    const uint32_t i = (blockIdx.x * kThreads + threadIdx.x) / (SPREAD ? 32 : 1);
+    const uint32_t i = SPREAD ? blockIdx.x * (kThreads / 32) + threadIdx.x / 32 : blockIdx.x * kThreads + threadIdx.x;
     uint32_t r, g;
     p.per_row.divmod(i < p.total ? i : p.total - 1, r, g);
     row = r;
@@ -61,6 +62,10 @@ __global__ void __launch_bounds__(kThreads) act8_store_kernel(const Act8Args p) 
     const int left = live ? p.channels - ch : 0;
     float v[16];
     load16<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, v);
+    if (sizeof(T) == 4 && !WITH_A && p.q != 0.f) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) v[i] = __int2float_rn(__float_as_int(v[i])) * p.q;
+    }
     keep16<SPREAD, CODE>(p.ck, row, ch, live, v);
     if constexpr (WITH_A) {
 #pragma unroll
@@ -212,11 +217,11 @@ template <class F> void by_type(const revnet_act_desc &d, bool spread, F &&f) {
 
 }  // namespace
 
-void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a) {
+void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a, float q) {
     const int size = d.dtype == REVNET_F32 ? 4 : 2, half = d.channels / 2;
     const bool gated = d.act == REVNET_ACT_SWIGLU && a;
     Act8Args p{};
-    p.x = x; p.a = a; p.ck = ck_view(ck, d.rows, d.channels);
+    p.x = x; p.a = a; p.ck = ck_view(ck, d.rows, d.channels); p.q = q;
     p.ld_x = d.ld_x; p.ld_a = d.ld_a;
     const double n = (double)d.rows * d.channels, out = a ? (gated ? n / 2 : n) * size : 0;
     const bool whole = rows_aligned(x, d.ld_x, size) && rows_aligned(a, d.ld_a, size) && (gated ? half : d.channels) % 32 == 0;

@@ -1,6 +1,7 @@
 // C ABI: context management and the block-level entry points.
 #include "common.cuh"
 #include "tc_ptx.cuh"
+#include "token.cuh"
 #include <string.h>
 #include <stdio.h>
 #include <math.h>
@@ -348,6 +349,72 @@ extern "C" int revnet_transition_bwd(revnet_ctx *ctx, const revnet_transition_de
     Exec ex = trans_exec(ctx, d, false, workspace, workspace_bytes, stream);
     trans_run(ex, d, true, in1, in2, W, gamma, beta, nullptr, nullptr, dout1, dout2, din1, din2, dW, dgamma, dbeta);
     return finish(ctx, ex, "revnet_transition_bwd");
+}
+
+// ---- the stored layer's input in 8 bits: one checkpoint, or one per half of a coupling state
+static int kept_parts(const revnet_transition_desc *d) { return d->in_split ? 2 : 1; }
+static size_t kept_part_bytes(const revnet_transition_desc *d) {
+    return (ck_bytes((int64_t)d->N * d->H * d->W, d->cin / kept_parts(d)) + 255) & ~size_t(255);
+}
+// what the backward call runs on: float32 inputs, decoded at the workspace's start
+static revnet_transition_desc kept_desc(const revnet_transition_desc *d) { revnet_transition_desc f = *d; f.state_frac_bits = 0; return f; }
+static size_t kept_input_bytes(const revnet_transition_desc *d) { return ((size_t)d->N * d->H * d->W * (d->cin / kept_parts(d)) * 4 + 255) & ~size_t(255); }
+static int check_kept(revnet_ctx *ctx, const revnet_transition_desc *d) {
+    int rc = check_trans(ctx, d);
+    if (rc) return rc;
+    if ((double)d->N * d->H * d->W * ck_pitch(d->cin) >= 34359738368.0) return fail(ctx, REVNET_E_UNSUPPORTED_SHAPE, "transition descriptor: too many input values for a checkpoint");
+    return REVNET_OK;
+}
+static revnet_act_desc kept_act(const revnet_transition_desc *d, int code) {
+    revnet_act_desc a{};
+    a.rows = (int64_t)d->N * d->H * d->W; a.channels = d->cin / kept_parts(d); a.dtype = REVNET_F32; a.code = code; a.act = REVNET_ACT_NONE;
+    a.ld_x = a.ld_a = a.channels;
+    return a;
+}
+extern "C" int revnet_transition_kept_bytes(revnet_ctx *ctx, const revnet_transition_desc *d, size_t *kept_bytes, size_t *bwd_workspace_bytes) {
+    int rc = check_kept(ctx, d);
+    if (rc) return rc;
+    if (kept_bytes) *kept_bytes = kept_parts(d) * kept_part_bytes(d);
+    if (bwd_workspace_bytes) {
+        const revnet_transition_desc f = kept_desc(d);
+        if ((rc = revnet_transition_workspace_bytes(ctx, &f, nullptr, bwd_workspace_bytes))) return rc;
+        *bwd_workspace_bytes += kept_parts(d) * kept_input_bytes(d);
+    }
+    return REVNET_OK;
+}
+extern "C" int revnet_transition_keep(revnet_ctx *ctx, const revnet_transition_desc *d, const void *in1, const void *in2, int code, void *kept, void *stream) {
+    int rc = check_kept(ctx, d);
+    if (rc) return rc;
+    if (!in1 || (d->in_split && !in2) || !kept || (code != REVNET_INT8 && code != REVNET_E4M3)) return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_keep: null pointer or unknown code");
+    if (!aligned16({in1, in2}) || ((uintptr_t)kept & 255)) return fail(ctx, REVNET_E_MISALIGNED, "revnet_transition_keep: inputs must be 16-byte, the buffer 256-byte aligned");
+    Exec ex = trans_exec(ctx, d, false, nullptr, 0, stream);
+    for (int i = 0; i < kept_parts(d); i++)
+        act8_store(ex, kept_act(d, code), i ? in2 : in1, (char *)kept + i * kept_part_bytes(d), nullptr, d->in_split ? ex.q : 0.f);
+    return finish(ctx, ex, "revnet_transition_keep");
+}
+extern "C" int revnet_transition_bwd_kept(revnet_ctx *ctx, const revnet_transition_desc *d, int code, const void *kept,
+                                          const float *dout1, const float *dout2, const float *W, const float *gamma, const float *beta,
+                                          float *din1, float *din2, float *dW, float *dgamma, float *dbeta,
+                                          void *workspace, size_t workspace_bytes, void *stream) {
+    size_t need = 0;
+    int rc = revnet_transition_kept_bytes(ctx, d, nullptr, &need);
+    if (rc) return rc;
+    if (!kept || !workspace || (code != REVNET_INT8 && code != REVNET_E4M3)) return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_bwd_kept: null pointer or unknown code");
+    if (((uintptr_t)kept & 255) || ((uintptr_t)workspace & 15)) return fail(ctx, REVNET_E_MISALIGNED, "revnet_transition_bwd_kept: the buffer must be 256-byte, the workspace 16-byte aligned");
+    if (workspace_bytes < need) return fail(ctx, REVNET_E_WORKSPACE_TOO_SMALL, "revnet_transition_bwd_kept: workspace too small");
+    const size_t part = kept_input_bytes(d), used = kept_parts(d) * part;
+    char *in1 = (char *)workspace, *in2 = d->in_split ? in1 + part : nullptr;
+    const revnet_transition_desc f = kept_desc(d);
+    // the pointers of the call are checked before anything is launched
+    if (!dout1 || !dout2 || !W || !gamma || !beta || !din1 || (d->in_split && !din2) || !dW || !dgamma || !dbeta)
+        return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_bwd_kept: null pointer");
+    if (!aligned16({dout1, dout2, W, gamma, beta, din1, din2, dW, dgamma, dbeta}))
+        return fail(ctx, REVNET_E_MISALIGNED, "revnet_transition_bwd_kept: pointers must be 16-byte aligned");
+    Exec ex = trans_exec(ctx, &f, false, nullptr, 0, stream);
+    for (int i = 0; i < kept_parts(d); i++)
+        act8_load(ex, kept_act(d, code), (const char *)kept + i * kept_part_bytes(d), i ? in2 : in1);
+    if ((rc = finish(ctx, ex, "revnet_transition_bwd_kept"))) return rc;
+    return revnet_transition_bwd(ctx, &f, in1, in2, dout1, dout2, W, gamma, beta, din1, din2, dW, dgamma, dbeta, (char *)workspace + used, workspace_bytes - used, stream);
 }
 
 // ---- device-side status

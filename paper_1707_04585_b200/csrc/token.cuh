@@ -23,7 +23,8 @@ static inline Checkpoint ck_view(const void *buf, int64_t rows, int channels) {
 static inline bool rows_aligned(const void *p, int64_t ld, int size) { return !p || (((uint64_t)(uintptr_t)p | (uint64_t)ld * size) & 31) == 0; }
 
 // ---------------------------------------------------------------- act8.cu, norm.cu, wgrad8.cu, logprobs.cu
-void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a);
+// q not 0: x is int32 fixed point with that step (float32 descriptor, a null)
+void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a, float q = 0.f);
 void act8_load(Exec &ex, const revnet_act_desc &d, const void *ck, void *a);
 void act8_bwd(Exec &ex, const revnet_act_desc &d, const void *ck, const void *da, void *dx, void *a_ck);
 void rmsnorm_fwd(Exec &ex, const revnet_norm_desc &d, const void *x, const void *r, const float *gamma, void *h, void *n, void *ck, float *rstd);

@@ -205,6 +205,8 @@ extern "C" int revnet_linear_wgrad(revnet_ctx *ctx, const revnet_wgrad_desc *des
     REFUSE(!dW || (d.rows > 0 && (!dy || !ck || !workspace)), REVNET_E_INVALID_ARG, "revnet_linear_wgrad: null pointer");
     REFUSE(!aligned(dW, 16) || !aligned(workspace, 16) || !aligned(ck, 256) || !aligned(dy, size_of(d.dy_dtype)) || !aligned(gamma, 4), REVNET_E_MISALIGNED,
            "revnet_linear_wgrad: dW and the workspace on 16 bytes, the checkpoint on 256, dy and gamma on their elements' size");
+    REFUSE(d.rows > 0 && d.dy_dtype == REVNET_BF16 && d.ld_dy % 8 == 0 && !aligned(dy, 16), REVNET_E_MISALIGNED,
+           "revnet_linear_wgrad: bf16 rows of dy a multiple of 16 bytes apart start on 16 bytes");
     REFUSE(d.rows > 0 && workspace_bytes < wgrad8_workspace(ctx, d), REVNET_E_WORKSPACE_TOO_SMALL, "revnet_linear_wgrad: workspace too small");
     if ((rc = check_device(ctx, "revnet_linear_wgrad: the context's device must be current"))) return rc;
     Exec ex = exec_of(ctx, stream);

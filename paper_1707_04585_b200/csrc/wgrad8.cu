@@ -8,7 +8,7 @@
 //   D      256 output channels x 256 input channels of fp32 in the pair's tensor memory, twice
 //
 // Long sums: the tensor cores round their running sum towards zero, an error that grows with the number of rows (7.8e-6 relative after about
-// 10000).  So a run of MMAs covers 1024 rows; the decoder warps then add its result to sums in registers (128 per thread), to nearest,
+// 10000).  So a run of MMAs covers 2048 rows; the decoder warps then add its result to sums in registers (128 per thread), to nearest,
 // while the MMAs of the next run fill the other half of tensor memory.
 //
 // Schedule: with P pairs resident, pair p takes the tiles p, p + P, ... as long as there is one for every pair, all of them at the same rows
@@ -26,7 +26,7 @@ constexpr int kGroups = 6, kGroupWarps = kDecoders / kGroups;    // every kGroup
 constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
 static_assert((4 + kDecoders) * kRegsFew + kSummers * kRegsSums == kThreads / 32 * kRegs, "the split is the launch's total");
 constexpr int kStep = 64;            // rows per step
-constexpr int kRun = 16;             // steps per run of the tensor cores' own sum
+constexpr int kRun = 32;             // steps per run of the tensor cores' own sum
 constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
 constexpr int kMaxPairs = 80;
 constexpr int kStepsMin = 8;         // a pair's share is at least that long where the work allows: shorter ones do not pay for their sums
@@ -392,9 +392,9 @@ template <int LANES, int QUADS> void sum_t(Exec &ex, const Wgrad8Args &a) {
 template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(const T *dy, int64_t ld, bool aligned, bf16 *out, int rows, int rows_step, int cout, int pitch, FastDiv groups) {
     pdl_enter();
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= (uint32_t)rows_step * groups.d) return;                     // (below 2^31, see the entry point)
     uint32_t row, g;
     groups.divmod(i, row, g);
-    if (row >= (uint32_t)rows_step) return;
     const int ch = (int)g * 8, n = row < (uint32_t)rows ? min(8, cout - ch) : 0;
     const T *src = dy + (size_t)row * ld + ch;
     float v[8];
@@ -430,6 +430,7 @@ struct Plan {
     int pitch;                       // elements per row of the prepared dy
     size_t prepared_bytes, partial_bytes;
 };
+// whether the loads can take dy from where it is (the entry point sees to its address)
 bool direct(const revnet_wgrad_desc &d) { return d.dy_dtype == REVNET_BF16 && d.ld_dy % 8 == 0; }
 Plan plan_of(const revnet_ctx *ctx, const revnet_wgrad_desc &d, bool prepared) {
     Plan w{};
@@ -477,14 +478,13 @@ template <int CODE> void run_t(Exec &ex, const Wgrad8Args &a, double bytes, doub
 }  // namespace
 
 size_t wgrad8_workspace(const revnet_ctx *ctx, const revnet_wgrad_desc &d) {
-    // whether dy can be loaded from where it is also depends on its address: the workspace serves either
-    const Plan w = plan_of(ctx, d, true);
+    const Plan w = plan_of(ctx, d, !direct(d));
     return w.prepared_bytes + w.partial_bytes + 256;
 }
 
 void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck, const float *gamma, float *dW, char *workspace) {
     if (d.rows == 0) { fill_zero(ex, dW, (size_t)d.cin * d.cout * 4); return; }
-    const bool prepared = !direct(d) || ((uintptr_t)dy & 15);
+    const bool prepared = !direct(d);
     const Plan w = plan_of(ex.ctx, d, prepared);
     const Checkpoint c = ck_view(ck, d.rows, d.cin);
     Wgrad8Args a{};

@@ -531,6 +531,29 @@ def test_offsets_beyond_32_bits(ctx):
         both(f)
 
 
+def test_more_rows_than_a_warp_each_can_be_counted_in_32_bits_of_threads(ctx):
+    """2^27 + 100 unaligned rows: a warp for each of them makes 2^32 threads."""
+    rows, ch = (1 << 27) + 100, 17
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("needs 40 GB")
+    x = torch.empty(rows, ch, dtype=torch.bfloat16, device="cuda").normal_()
+    ck = torch.empty(B.revnet_act_ckpt_bytes(ctx, rows, ch), dtype=torch.uint8, device="cuda")
+    y = torch.zeros_like(x)
+    d = B.act_desc(rows, ch, "bf16")
+    B.revnet_act_store(ctx, d, x, ck)
+    B.revnet_act_load(ctx, d, ck, y)
+    for part in (slice(0, 50), slice(rows - 150, rows), slice(rows // 2, rows // 2 + 50)):
+        c, s = ref.encode(x[part].cpu().double().numpy(), "int8")
+        assert torch.equal(y[part].cpu().double(), ref.decode(c, s, ch, "int8"))
+    assert ((y - x).abs().amax() <= x.abs().amax() / 127).item()
+    n, rs = torch.zeros_like(x), torch.empty(rows, device="cuda")
+    B.revnet_rmsnorm_fwd(ctx, B.norm_desc(rows, ch, "bf16", "bf16"), x, None, None, None, n, None, rs)
+    for part in (slice(0, 50), slice(rows - 50, rows)):
+        want, _, wn = ref.norm_fwd(x[part].cpu().double(), 1.0, 1e-5)
+        within(rs[part].cpu().double(), want, ROW * want)
+        within(n[part].cpu().double(), wn, (ROW + 3 * U) * wn.abs(), "bf16")
+
+
 def pipeline(ctx, p, s):
     """A residual function over tokens as a user runs it: forward, loss, backward from what was kept in 8 bits.  `s` owns every buffer."""
     T, C, H, V = p["T"], p["C"], p["H"], p["V"]
@@ -649,6 +672,45 @@ def test_captured_calls_and_other_streams(ctx):
     got = taken(sets[0][1])
     assert all(torch.equal(got[k], want[1][k]) for k in got)
     del graphs
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("mode,frac,split,cin,k,stride", [(0, 16, 1, 64, 3, 2), (0, 0, 1, 24, 1, 1), (1, 0, 0, 20, 3, 1), (0, 12, 0, 32, 3, 2), (1, 16, 1, 8, 1, 2)])
+def test_stored_layer_from_its_kept_input(ctx, mode, frac, split, cin, k, stride, code):
+    """revnet_transition_bwd_kept has the bits of revnet_transition_bwd on the values that were kept, and these are the format's."""
+    N, H, cout = 3, 10, 32
+    d = B.TransitionDesc(N, H, H, cin, cout, k, stride, split, 1e-5, mode, frac)
+    g = torch.Generator().manual_seed(cin + k)
+    halves, c = (2, cin // 2) if split else (1, cin)
+    x = [torch.randn(N * H * H, c, generator=g) * 2 for _ in range(halves)]
+    fixed = frac and split           # (a plain input is float32 whatever the state's format)
+    raw = [torch.round(t.double() * 2 ** frac).to(torch.int32) if fixed else t for t in x]
+    val = [t.double() / 2 ** frac if fixed else t.double() for t in raw]
+    dev = [t.cuda() for t in raw] + [None] * (2 - halves)
+    kept_bytes, ws_bytes = B.revnet_transition_kept_bytes(ctx, d)
+    kept = torch.full((kept_bytes,), 0xA5, dtype=torch.uint8, device="cuda")
+    B.revnet_transition_keep(ctx, d, *dev, code, kept)
+    part = kept_bytes // halves
+    x8 = []
+    for i, t in enumerate(val):
+        wc, ws = ref.encode(t.float().double().numpy(), code)
+        gc, gs = ref.take_apart(kept[i * part:], N * H * H, c)
+        assert (gs == ws).all() and (ref.code_values(gc, code) == ref.code_values(wc, code)).all()
+        x8.append(ref.decode(wc, ws, c, code).float().cuda())
+    W = (torch.randn(cout, k, k, cin, generator=g) * (2 / (cin * k * k)) ** 0.5).cuda()
+    gamma, beta = (1 + 0.1 * torch.randn(cin, generator=g)).cuda(), (0.1 * torch.randn(cin, generator=g)).cuda()
+    out = N * (-(-H // stride)) ** 2
+    dout = [torch.randn(out, cout // 2, generator=g).cuda() for _ in range(2)]
+
+    def grads():
+        return [torch.empty(N * H * H, c, device="cuda") for _ in range(halves)] + [None] * (2 - halves) + [torch.empty_like(W), torch.empty_like(gamma), torch.empty_like(beta)]
+    got, want = grads(), grads()
+    B.revnet_transition_bwd_kept(ctx, d, code, kept, *dout, W, gamma, beta, *got, torch.empty(ws_bytes, dtype=torch.uint8, device="cuda"))
+    f = B.TransitionDesc(N, H, H, cin, cout, k, stride, split, 1e-5, mode, 0)
+    ws = torch.empty(B.revnet_transition_workspace_bytes(ctx, f)[1], dtype=torch.uint8, device="cuda")
+    B.revnet_transition_bwd(ctx, f, *(x8 + [None] * (2 - halves)), *dout, W, gamma, beta, *want, ws)
+    for a, b in zip(got, want):
+        assert a is None or torch.equal(a, b)
 
 
 def test_refusals_on_the_device(ctx):

@@ -165,8 +165,12 @@ def test_wgrad_pointers_and_workspace(ctx):
     assert call(ctx, "revnet_linear_wgrad", d, FAKE, FAKE, 0, FAKE, ws=(0, need)) == INVALID
     for args, ws in (((FAKE + 1, FAKE, 0, FAKE), FAKE), ((FAKE, FAKE + 16, 0, FAKE), FAKE), ((FAKE, FAKE, 0, FAKE + 4), FAKE), ((FAKE, FAKE, 0, FAKE), FAKE + 4)):
         assert call(ctx, "revnet_linear_wgrad", d, *args, ws=(ws, need)) == MISALIGNED
-    # a training batch: the parts of the tiles that the SMs share are bounded, whatever the sizes
-    assert B.revnet_linear_wgrad_workspace_bytes(ctx, B.wgrad_desc(16384, 4096, 4096)) <= 16384 * 4096 * 2 + (160 << 20)
+    d.ld_dy = 32                     # bf16 rows that the loads take from where they are
+    need = B.revnet_linear_wgrad_workspace_bytes(ctx, d)
+    assert call(ctx, "revnet_linear_wgrad", d, FAKE + 8, FAKE, 0, FAKE, ws=(FAKE, need)) == MISALIGNED
+    # the parts of the tiles that the SMs share are bounded, whatever the sizes; only other rows are laid out anew
+    assert B.revnet_linear_wgrad_workspace_bytes(ctx, B.wgrad_desc(1 << 20, 4096, 4096)) <= 160 << 20
+    assert (1 << 20) * 4096 * 2 < B.revnet_linear_wgrad_workspace_bytes(ctx, B.wgrad_desc(1 << 20, 4096, 4096, ld_dy=4097)) <= (1 << 20) * 4096 * 2 + (160 << 20)
 
 
 BAD_LOGP = [(dict(rows=-1), INVALID), (dict(dtype=2), INVALID), (dict(vocab=0), SHAPE), (dict(vocab=(1 << 24) + 1), SHAPE), (dict(rows=1 << 31), SHAPE),
@@ -191,6 +195,29 @@ def test_logprob_pointers(ctx):
                  (FAKE, FAKE, FAKE, 0, FAKE, FAKE, FAKE), (FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0)):
         assert call(ctx, "revnet_logprobs_bwd", d, *args) == INVALID
     assert call(ctx, "revnet_logprobs_bwd", d, FAKE, FAKE + 1, FAKE, FAKE, FAKE, FAKE, FAKE) == MISALIGNED
+
+
+def test_kept_input_of_a_stored_layer(ctx):
+    d = B.TransitionDesc(2, 6, 6, 16, 24, 3, 2, 1, 1e-5, 0, 16)
+    kept, ws = B.revnet_transition_kept_bytes(ctx, d)
+    assert kept == 2 * ((B._ck_bytes(72, 8) + 255) // 256 * 256)
+    assert ws >= B.revnet_transition_workspace_bytes(ctx, d)[1] + 72 * 16 * 4
+    big = B.TransitionDesc(64, 28, 28, 2048, 4096, 3, 2, 1, 1e-5, 0, 16)
+    assert B.revnet_transition_kept_bytes(ctx, big)[0] <= 0.27 * 64 * 28 * 28 * 2048 * 4          # of the float32 or fixed-point pair
+    lib, P = B.lib(), C.c_void_p
+
+    def keep(*p, code=0):
+        return lib.revnet_transition_keep(ctx.h, C.byref(d), P(p[0]), P(p[1]), C.c_int(code), P(p[2]), P(0))
+
+    def bwd(kept_at=FAKE, code=0, size=ws, at=FAKE, **other):
+        p = [P(other.get(n, FAKE)) for n in ("dout1", "dout2", "W", "gamma", "beta", "din1", "din2", "dW", "dgamma", "dbeta")]
+        return lib.revnet_transition_bwd_kept(ctx.h, C.byref(d), C.c_int(code), P(kept_at), *p, P(at), C.c_size_t(size), P(0))
+    assert keep(0, FAKE, FAKE) == INVALID and keep(FAKE, 0, FAKE) == INVALID and keep(FAKE, FAKE, 0) == INVALID and keep(FAKE, FAKE, FAKE, code=2) == INVALID
+    assert keep(FAKE + 4, FAKE, FAKE) == MISALIGNED and keep(FAKE, FAKE, FAKE + 16) == MISALIGNED
+    assert bwd(kept_at=0) == INVALID and bwd(code=-1) == INVALID and bwd(din2=0) == INVALID and bwd(dW=0) == INVALID
+    assert bwd(size=ws - 1) == SMALL and bwd(kept_at=FAKE + 32) == MISALIGNED and bwd(dout1=FAKE + 4) == MISALIGNED
+    d.k = 5
+    assert keep(FAKE, FAKE, FAKE) == SHAPE and bwd() == SHAPE
 
 
 def test_binding_checks_tensors_before_their_addresses(ctx):
