@@ -423,9 +423,12 @@ void logprobs_bwd(Exec &ex, const revnet_logprob_desc &d, const void *logits, co
     p.rows = d.rows; p.ld = d.ld; p.vocab = d.vocab; p.status = ex.ctx->dev_status;
     unsigned threads = 32;
     while (threads < 256 && (int)threads * kVec < d.vocab) threads *= 2;
-    p.chunk = (int)threads * kVec * 2;
-    int64_t chunks = (d.vocab + p.chunk - 1) / p.chunk;
-    while (chunks > 1 && d.rows * chunks >= (int64_t(1) << 31)) { p.chunk *= 2; chunks = (d.vocab + p.chunk - 1) / p.chunk; }
+    // about four vectors per thread (two: 4 % slower, one: 25 %), rows cut into equal parts (of whole vectors, so that they stay aligned)
+    const int per = (int)threads * kVec * 4;
+    int64_t chunks = (d.vocab + per - 1) / per;
+    while (chunks > 1 && d.rows * chunks >= (int64_t(1) << 31)) chunks = (chunks + 1) / 2;
+    p.chunk = (int)(((d.vocab + chunks - 1) / chunks + kVec - 1) / kVec * kVec);
+    chunks = (d.vocab + p.chunk - 1) / p.chunk;
     p.chunks = fast_div((uint32_t)chunks);
     const double bytes = (double)d.rows * d.vocab * (d.dtype == REVNET_F32 ? 8 : 4);
     const unsigned grid = (unsigned)(d.rows * chunks);

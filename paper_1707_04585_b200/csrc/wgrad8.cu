@@ -446,6 +446,8 @@ Plan plan_of(const revnet_ctx *ctx, const revnet_wgrad_desc &d, bool prepared) {
     w.rest = w.tiles - w.waves * w.pairs;
     w.sharers = sharers_of(w.rest);
     if (w.rest && w.steps - (int64_t)w.rest * w.steps / w.sharers < kSplitSteps) w.sharers = w.rest;         // one more round of whole tiles
+    // the same number of pairs for every tile where that leaves few of them idle: no pair then has two parts to add and store
+    else if (w.rest && w.sharers / w.rest * w.rest >= w.sharers * 85 / 100) w.sharers -= w.sharers % w.rest;
     w.pitch = (d.cout + 7) & ~7;
     w.prepared_bytes = prepared ? ((size_t)w.steps * kStep * w.pitch * 2 + 255) & ~size_t(255) : 0;
     w.partial_bytes = w.rest == 0 || w.rest % w.sharers == 0 ? 0 : (size_t)w.sharers * 2 * kSlot * 4;        // (a multiple: whole tiles for all of them)
