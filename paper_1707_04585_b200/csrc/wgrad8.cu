@@ -16,6 +16,7 @@
 // getting [p n / P', (p + 1) n / P').  Parts of a tile go to the workspace, and a second kernel adds them in a fixed order.
 #include "token.cuh"
 #include "tc_ptx.cuh"
+#include <algorithm>
 
 namespace {
 using namespace tc;
@@ -29,7 +30,7 @@ constexpr int kStep = 64;            // rows per step
 constexpr int kRun = 32;             // steps per run of the tensor cores' own sum
 constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
 constexpr int kMaxPairs = 80;
-constexpr int kStepsMin = 8;         // a pair's share is at least that long where the work allows: shorter ones do not pay for their sums
+constexpr int kStepsMin = 8;         // a pair's share of a tile is at least that long: shorter ones do not pay for their sums
 constexpr int kSplitSteps = 32;      // tiles are cut only where that saves as many steps: parts have to be written, read and added (8192 rows, 4096 x 1024:
                                      // 78 us cut, 62 whole)
 constexpr uint32_t kBlock = 64 * 128;        // bytes of 64 rows x 64 channels of bf16, the unit of both operands
@@ -61,7 +62,7 @@ struct alignas(64) Wgrad8Args {
     int begin[kMaxPairs + 1];        // first of the steps left over that pair q works on (below 2^31: at most 79 tiles of fewer than 3 * 2^23 steps)
     uint8_t first[kMaxPairs], last[kMaxPairs];       // of a tile left over: the pairs that work on it
     uint32_t rows_pad;
-    int vec;                         // dW rows take stores of 32 (2) or 16 bytes (1)
+    int vec;                         // dW rows take stores of 16 bytes
 };
 // The pieces of work of a pair, in order; every role of both CTAs walks the same list.
 struct Pieces {
@@ -245,35 +246,39 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
                 if (lane == 0) mbar_arrive_remote(d_empty0 + 8u * buf);
             }
             const int r = (int)rank * 128 + quarter * 32 + lane, o = (job.tile / p.tiles_c) * kM + r;
-            const int c0 = (job.tile % p.tiles_c) * kN + half * 128, left = ok && o < p.cout ? p.cin - c0 : 0;
+            const int c0 = (job.tile % p.tiles_c) * kN + half * 128;
             if (job.slot >= 0) {
                 // a part: [column quad][row][4], so that a warp's 32 rows are one run of 512 bytes
+                const int left = ok && o < p.cout ? p.cin - c0 : 0;
                 float4 *part = reinterpret_cast<float4 *>(p.partial + (size_t)job.slot * kSlot) + (size_t)half * 32 * kM + r;
 #pragma unroll
                 for (int i = 0; i < 128; i += 4)
                     if (i < left) part[(size_t)(i / 4) * kM] = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
                 continue;
             }
-            float *out = p.dW + (size_t)o * p.cin + c0;
-            if (p.gamma) {
-                const float *g = p.gamma + c0;
+            // a tile: 32 x 32 squares transposed in registers, so that a store is 128 consecutive bytes of a row, whatever the row's alignment (24 rows,
+            // 1682 x 3709: 180 us with every lane writing its own row)
+            if (!ok) break;
+            const int rows = p.cout - (o - lane);
 #pragma unroll
-                for (int i = 0; i < 128; i++) if (i < left) sum[i] *= g[i];
-            }
-            if (p.vec == 2 && left >= 128) {
+            for (int c = 0; c < 128; c += 32) {
+                if (c0 + c >= p.cin || rows <= 0) break;                 // the same for the whole warp
 #pragma unroll
-                for (int i = 0; i < 128; i += 8) {
-                    uint32_t t[8];
+                for (int s = 16; s; s >>= 1)
 #pragma unroll
-                    for (int e = 0; e < 8; e++) t[e] = __float_as_uint(sum[i + e]);
-                    st8(out + i, t, true);
+                    for (int j = 0; j < 32; j++)
+                        if ((j & s) == 0) {
+                            const bool up = (lane & s) != 0;
+                            const float got = __shfl_xor_sync(0xffffffffu, up ? sum[c + j] : sum[c + j + s], s);
+                            if (up) sum[c + j] = got; else sum[c + j + s] = got;
+                        }
+                if (c + lane < p.cin - c0) {
+                    const float g = p.gamma ? p.gamma[c0 + c + lane] : 1.f;
+                    float *out = p.dW + (size_t)(o - lane) * p.cin + c0 + c + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; j++)
+                        if (j < rows) out[(size_t)j * p.cin] = sum[c + j] * g;
                 }
-            } else if (p.vec) {
-#pragma unroll
-                for (int i = 0; i < 128; i += 4) if (i < left) *reinterpret_cast<float4 *>(out + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 128; i++) if (i < left) out[i] = sum[i];
             }
         }
     } else {
@@ -388,7 +393,8 @@ template <int LANES, int QUADS> void sum_t(Exec &ex, const Wgrad8Args &a) {
 }
 
 // dy for the loads: rows of `pitch` bf16 on 16-byte boundaries.  float32 becomes three parts, the bits of a value 8 at a time: their sum is the
-// value (infinities and NaN stay in the first).  Rows of the last step behind the last one are zeros between the parts.
+// value (infinities and NaN stay in the upper one).  The lowest part comes first: the tensor cores cut small products off at the last bits of
+// the sum that they are added to, which should be small then (330 rows: error 1.7e-6 with the upper part first).  Rows of the last step behind the last one are zeros between the parts.
 template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(const T *dy, int64_t ld, bool aligned, bf16 *out, int rows, int rows_step, int cout, int pitch, FastDiv groups) {
     pdl_enter();
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
@@ -421,7 +427,7 @@ template <class T> __global__ void __launch_bounds__(256) wgrad8_prepare_kernel(
             v[j] = finite ? v[j] - __uint_as_float(b) : 0.f;
             if (j & 1) w[j >> 1] |= b; else w[j >> 1] = b >> 16;
         }
-        *reinterpret_cast<uint4 *>(out + ((size_t)part * rows_step + row) * pitch + ch) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4 *>(out + ((size_t)(sizeof(T) == 4 ? 2 - part : 0) * rows_step + row) * pitch + ch) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -439,7 +445,8 @@ Plan plan_of(const revnet_ctx *ctx, const revnet_wgrad_desc &d, bool prepared) {
     w.tiles_c = (d.cin + kN - 1) / kN;
     w.tiles = w.tiles_c * ((d.cout + kM - 1) / kM);
     const int most = ctx->sm_count / 2 < kMaxPairs ? ctx->sm_count / 2 : kMaxPairs;
-    auto sharers_of = [&](int64_t tiles) { const int64_t q = (tiles * w.steps + kStepsMin - 1) / kStepsMin; return (int)(q < most ? q : most); };
+    // a pair for every kStepsMin steps, and for every tile however short
+    auto sharers_of = [&](int64_t tiles) { const int64_t q = std::max(tiles, (tiles * w.steps + kStepsMin - 1) / kStepsMin); return (int)std::min<int64_t>(w.steps ? q : 0, most); };
     w.pairs = sharers_of(w.tiles);
     if (w.tiles < w.pairs && w.steps - (int64_t)w.tiles * w.steps / w.pairs < kSplitSteps) w.pairs = w.tiles;
     w.waves = w.pairs ? w.tiles / w.pairs : 0;
@@ -492,7 +499,7 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     Wgrad8Args a{};
     a.scales = c.scales; a.gamma = gamma; a.dW = dW; a.partial = (float *)(workspace + w.prepared_bytes); a.status = ex.ctx->dev_status;
     a.rows = (int)d.rows; a.cin = d.cin; a.cout = d.cout; a.row_steps = w.row_steps; a.steps = w.steps; a.tiles_c = w.tiles_c;
-    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = rows_aligned(dW, d.cin, 4) ? 2 : (d.cin % 4 == 0 ? 1 : 0);       // (dW itself is on 16 bytes)
+    a.pairs = w.pairs; a.waves = w.waves; a.rest = w.rest; a.sharers = w.sharers; a.rows_pad = c.rows_pad; a.vec = d.cin % 4 == 0;        // (dW itself is on 16 bytes)
     for (int q = 0; q <= w.sharers; q++) a.begin[q] = w.sharers ? (int)((int64_t)w.rest * w.steps * q / w.sharers) : 0;
     for (int t = 0, q = 0; t < w.rest; t++) {
         while (a.begin[q + 1] <= t * w.steps) q++;
