@@ -3,9 +3,10 @@
 //   store  ck = checkpoint of x, a = act(x)          load  a = act(x8)          bwd  dx = da act'(x8), checkpoint of act(x8)
 //
 // Every value is read and written once, so HBM bounds all of them.  A thread owns 16 channels (token.cuh): consecutive ones where rows are
-// aligned whole blocks, the amax of a block of 32 being one shuffle between two lanes; spread over a warp's 512 elsewhere.  No shared memory and no second
+// aligned, the amax of a block of 32 being one shuffle between two lanes; spread over a warp's 512 elsewhere.  No shared memory and no second
 // pass.  Flat indexing over (row, group), since rows of any length then leave no thread idle but in the last CTA.
 #include "token.cuh"
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -41,6 +42,7 @@ struct Act8Args {
     int64_t ld_x, ld_a;              // of x, a above
     uint32_t total;                  // groups (SPREAD: warps' 512 channels) in all
     FastDiv per_row;                 // of a row
+    bool wide;                       // 32-byte accesses (token.cuh)
     float q;                         // not 0: x is int32 fixed point, value = i * q (a coupling state)
 };
 
@@ -61,7 +63,7 @@ __global__ void __launch_bounds__(kThreads) act8_store_kernel(const Act8Args p) 
     const bool live = place<SPREAD>(p, row, ch);
     const int left = live ? p.channels - ch : 0;
     float v[16];
-    load16<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, v);
+    load16<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, p.wide, v);
     if (sizeof(T) == 4 && !WITH_A && p.q != 0.f) {
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = __int2float_rn(__float_as_int(v[i])) * p.q;
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(kThreads) act8_store_kernel(const Act8Args p) 
     if constexpr (WITH_A) {
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = act<ACT>(v[i]);
-        store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, v);
+        store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, p.wide, v);
     }
 }
 // gated, halves in whole blocks of 32 (CODE -1: without the checkpoint, halves of any length): the thread that needs g and u for a encodes both
@@ -83,8 +85,8 @@ __global__ void __launch_bounds__(kThreads) act8_store_gated_kernel(const Act8Ar
     float g[16], u[16];
     Raw16<T> rg, ru;
     const T *x = (const T *)p.x + row * p.ld_x + ch;
-    load_raw<SPREAD>(x, left, rg);
-    load_raw<SPREAD>(x + p.half, left, ru);
+    load_raw<SPREAD>(x, left, p.wide, rg);
+    load_raw<SPREAD>(x + p.half, left, p.wide, ru);
     unpack(rg, g); unpack(ru, u);
     if constexpr (CODE >= 0) {
         keep16<SPREAD, CODE>(p.ck, row, ch, live, g, p.half);            // the first half ends where the second begins
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(kThreads) act8_store_gated_kernel(const Act8Ar
     }
 #pragma unroll
     for (int i = 0; i < 16; i++) g[i] = act<REVNET_ACT_SILU>(g[i]) * u[i];
-    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, g);
+    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, p.wide, g);
 }
 
 template <bool SPREAD, class T, int CODE, int ACT>
@@ -117,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) act8_load_kernel(const Act8Args p) {
 #pragma unroll
         for (int i = 0; i < 16; i++) v[i] = act<ACT>(v[i]);
     }
-    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, v);
+    store16<SPREAD>((T *)p.a + row * p.ld_a + ch, left, p.wide, v);
 }
 
 template <bool SPREAD, class T, int CODE, int ACT>
@@ -129,7 +131,7 @@ __global__ void __launch_bounds__(kThreads) act8_bwd_kernel(const Act8Args p) {
     float x[16], da[16];
     Raw16<T> rd;
     RawCodes<SPREAD> rx, ru;
-    load_raw<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, rd);
+    load_raw<SPREAD>((const T *)p.x + row * p.ld_x + ch, left, p.wide, rd);
     load_codes<SPREAD>(p.ck, row, ch, left, rx);
     if constexpr (ACT == REVNET_ACT_SWIGLU) load_codes<SPREAD>(p.ck, row, p.half + ch, left, ru);
     unpack(rd, da);
@@ -146,8 +148,8 @@ __global__ void __launch_bounds__(kThreads) act8_bwd_kernel(const Act8Args p) {
             u[i] *= s;                               // (codes that were not loaded are zeros, as the padding of the checkpoint has to be)
             da[i] *= s;
         }
-        store16<SPREAD>(dx, left, x);
-        store16<SPREAD>(dx + p.half, left, da);
+        store16<SPREAD>(dx, left, p.wide, x);
+        store16<SPREAD>(dx + p.half, left, p.wide, da);
         if (p.out.codes) keep16<SPREAD, CODE>(p.out, row, ch, live, u);
     } else {
 #pragma unroll
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) act8_bwd_kernel(const Act8Args p) {
             da[i] = ACT == REVNET_ACT_RELU && !(x[i] > 0.f) && x[i] == x[i] ? 0.f : da[i] * d;      // an infinite gradient stops at a closed ReLU too
             x[i] = a;
         }
-        store16<SPREAD>(dx, left, da);
+        store16<SPREAD>(dx, left, p.wide, da);
         if (p.out.codes) keep16<SPREAD, CODE>(p.out, row, ch, live, x);
     }
 }
@@ -224,16 +226,19 @@ void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, voi
     p.x = x; p.a = a; p.ck = ck_view(ck, d.rows, d.channels); p.q = q;
     p.ld_x = d.ld_x; p.ld_a = d.ld_a;
     const double n = (double)d.rows * d.channels, out = a ? (gated ? n / 2 : n) * size : 0;
-    const bool whole = rows_aligned(x, d.ld_x, size) && rows_aligned(a, d.ld_a, size) && (gated ? half : d.channels) % 32 == 0;
+    // (a gated row's second half starts on a block's boundary here, so on 32 bytes too)
+    const int access = std::min(row_access(x, d.ld_x, size, d.channels), row_access(a, d.ld_a, size, gated ? half : d.channels));
+    p.wide = access == 2;
     if (!gated || half % 32 == 0) {
-        if (!fill(p, d, gated ? half : d.channels, !whole)) return;
-        by_type(d, !whole, [&](auto s, auto t, auto c) { store_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, n * (size + 1) + out); });
+        if (!fill(p, d, gated ? half : d.channels, !access)) return;
+        by_type(d, !access, [&](auto s, auto t, auto c) { store_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, n * (size + 1) + out); });
         return;
     }
     // halves that end inside a block: the checkpoint first, then the activation alone
     Act8Args only = p;
     only.a = nullptr;
-    const bool first = rows_aligned(x, d.ld_x, size) && d.channels % 32 == 0;
+    const int first = row_access(x, d.ld_x, size, d.channels);
+    only.wide = first == 2;
     if (!fill(only, d, d.channels, !first)) return;
     by_type(d, !first, [&](auto s, auto t, auto c) { store_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, only, d, n * (size + 1)); });
     fill(p, d, half, true);
@@ -247,10 +252,12 @@ void act8_load(Exec &ex, const revnet_act_desc &d, const void *ck, void *a) {
     Act8Args p{};
     p.a = a; p.ck = ck_view(ck, d.rows, d.channels);
     p.ld_a = d.ld_a;
-    const bool whole = rows_aligned(a, d.ld_a, size) && out % 32 == 0;
-    if (!fill(p, d, out, !whole)) return;
+    // codes of a gated row's second half: 16 bytes on 16-byte boundaries under one scale, or one by one
+    const int access = d.act == REVNET_ACT_SWIGLU && out % 16 ? 0 : row_access(a, d.ld_a, size, out);
+    p.wide = access == 2;
+    if (!fill(p, d, out, !access)) return;
     const double bytes = (double)d.rows * (d.channels + (double)p.half * size);
-    by_type(d, !whole, [&](auto s, auto t, auto c) { load_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
+    by_type(d, !access, [&](auto s, auto t, auto c) { load_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
 }
 
 void act8_bwd(Exec &ex, const revnet_act_desc &d, const void *ck, const void *da, void *dx, void *a_ck) {
@@ -258,8 +265,9 @@ void act8_bwd(Exec &ex, const revnet_act_desc &d, const void *ck, const void *da
     Act8Args p{};
     p.x = da; p.a = dx; p.ck = ck_view(ck, d.rows, d.channels); p.out = ck_view(a_ck, d.rows, out);
     p.ld_x = d.ld_a; p.ld_a = d.ld_x;
-    const bool whole = rows_aligned(da, d.ld_a, size) && rows_aligned(dx, d.ld_x, size) && out % 32 == 0;
-    if (!fill(p, d, out, !whole)) return;
+    const int access = d.act == REVNET_ACT_SWIGLU && out % 16 ? 0 : std::min(row_access(da, d.ld_a, size, out), row_access(dx, d.ld_x, size, d.channels));
+    p.wide = access == 2;
+    if (!fill(p, d, out, !access)) return;
     const double bytes = (double)d.rows * (d.channels * (1.0 + size) + out * (size + (a_ck ? 1.0 : 0.0)));
-    by_type(d, !whole, [&](auto s, auto t, auto c) { bwd_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
+    by_type(d, !access, [&](auto s, auto t, auto c) { bwd_t<decltype(s)::value, decltype(t), decltype(c)::value>(ex, p, d, bytes); });
 }

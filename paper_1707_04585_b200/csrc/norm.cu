@@ -7,8 +7,9 @@
 // (backward: that and the sum of gamma dn h) is one reduction over the row, and everything else is local to a thread's 16 channels
 // (token.cuh).  A row belongs to `tpr` threads, a power of two: up to 32 of them reduce by shuffles, more through shared memory.  Short
 // rows share a CTA.  CTAs are resident and walk over the rows; while one row is reduced and written, the next ones are on their way into
-// shared memory (up to 8192 channels of whole blocks on 32-byte boundaries; others are loaded when they are needed).
+// shared memory (up to 8192 channels of rows in 16-byte pieces; others are loaded when they are needed).
 #include "token.cuh"
+#include <algorithm>
 #include <type_traits>
 
 namespace {
@@ -23,12 +24,13 @@ struct NormArgs {
     int channels;
     int tpr_log;                     // threads per row
     int ck_scaled;
+    bool wide;                       // 32-byte accesses (token.cuh)
     float eps, inv_c;
 };
 
 // gamma of a thread's channels (ones where there is none, zeros behind the row's end)
 template <bool SPREAD> __device__ __forceinline__ void load_gamma(const NormArgs &p, int ch, float (&g)[16]) {
-    if (p.gamma) { load16<SPREAD>(p.gamma + ch, p.channels - ch, g); return; }
+    if (p.gamma) { load16<SPREAD>(p.gamma + ch, p.channels - ch, p.wide, g); return; }
 #pragma unroll
     for (int i = 0; i < 16; i++) g[i] = ch + step_of<SPREAD>(i) < p.channels ? 1.f : 0.f;
 }
@@ -111,8 +113,8 @@ __global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kCh
                 fetched(from + mine * kX, lane, x);
                 if (p.r) fetched(from + kX * THREADS + mine * kChunks<TB>, lane, r);
             } else {
-                load_raw<SPREAD>((const TS *)p.x + (at_s + ch), left, x);
-                if (p.r) load_raw<SPREAD>((const TB *)p.r + (at_b + ch), left, r);
+                load_raw<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x);
+                if (p.r) load_raw<SPREAD>((const TB *)p.r + (at_b + ch), left, p.wide, r);
             }
             unpack(x, h[s]);
             if (p.r) {
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kCh
                 for (int i = 0; i < 16; i++) h[s][i] += add[i];
                 pack(h[s], x);                       // the norm is of h as it is stored, so that the backward pass sees the same h
                 unpack(x, h[s]);
-                if (p.h) store_raw<SPREAD>((TS *)p.h + (at_s + ch), left, x);
+                if (p.h) store_raw<SPREAD>((TS *)p.h + (at_s + ch), left, p.wide, x);
             }
 #pragma unroll
             for (int i = 0; i < 16; i++) sum[0] = fmaf(h[s][i], h[s][i], sum[0]);
@@ -144,7 +146,7 @@ __global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kCh
             if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
 #pragma unroll
             for (int i = 0; i < 16; i++) { h[s][i] *= rstd; n[i] = h[s][i] * gamma[i]; }
-            if (p.n) store16<SPREAD>((TB *)p.n + (at_b + ch), left, n);
+            if (p.n) store16<SPREAD>((TB *)p.n + (at_b + ch), left, p.wide, n);
             if (p.ck.codes) {
                 if (p.ck_scaled) keep16<SPREAD, CODE>(p.ck, row, ch, row_ok, n);
                 else keep16<SPREAD, CODE>(p.ck, row, ch, row_ok, h[s]);
@@ -219,8 +221,8 @@ __global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kern
                     unpack(rx, x[s]);
                 } else decode16<CODE>(from[(kS + kB) * THREADS + threadIdx.x], byte_next, x[s]);
             } else {
-                load16<SPREAD>((const TB *)p.dn + (at_b + ch), left, dn[s]);
-                if constexpr (FROM_H) load16<SPREAD>((const TS *)p.x + (at_s + ch), left, x[s]);
+                load16<SPREAD>((const TB *)p.dn + (at_b + ch), left, p.wide, dn[s]);
+                if constexpr (FROM_H) load16<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x[s]);
                 else read16<SPREAD, CODE>(p.ck, row, ch, left, x[s]);
                 if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
             }
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kern
             if (p.dh) {
                 Raw16<TS> rh;
                 if constexpr (kAsync) fetched(from + mine * kS, lane, rh);
-                else load_raw<SPREAD>((const TS *)p.dh + (at_s + ch), left, rh);
+                else load_raw<SPREAD>((const TS *)p.dh + (at_s + ch), left, p.wide, rh);
                 unpack(rh, d);
             } else {
 #pragma unroll
@@ -270,8 +272,8 @@ __global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kern
                 }
                 d[i] = fmaf(x[s][i], back, d[i] + w);
             }
-            store16<SPREAD>((TS *)p.dx + (at_s + ch), left, d);
-            if (p.dr) store16<SPREAD>((TB *)p.dr + (at_b + ch), left, d);
+            store16<SPREAD>((TS *)p.dx + (at_s + ch), left, p.wide, d);
+            if (p.dr) store16<SPREAD>((TB *)p.dr + (at_b + ch), left, p.wide, d);
         }
         if (SLOTS > 1) load_gamma<SPREAD>(p, ch0, gamma);
     }
@@ -388,8 +390,10 @@ void rmsnorm_fwd(Exec &ex, const revnet_norm_desc &d, const void *x, const void 
     const int ss = d.stream_dtype == REVNET_F32 ? 4 : 2, sb = d.branch_dtype == REVNET_F32 ? 4 : 2;
     NormArgs p = args_of(d);
     p.x = x; p.r = r; p.gamma = gamma; p.h = h; p.n = n; p.rstd = rstd; p.ck = ck_view(ck, d.rows, d.channels);
-    const bool spread = d.channels % 32 || !rows_aligned(x, d.ld_stream, ss) || !rows_aligned(h, d.ld_stream, ss) || !rows_aligned(r, d.ld_branch, sb) ||
-                        !rows_aligned(n, d.ld_branch, sb) || !rows_aligned(gamma, 0, 4);
+    const int access = std::min({row_access(x, d.ld_stream, ss, d.channels), row_access(h, d.ld_stream, ss, d.channels), row_access(r, d.ld_branch, sb, d.channels),
+                                 row_access(n, d.ld_branch, sb, d.channels), row_access(gamma, 0, 4, d.channels)});
+    const bool spread = access == 0;
+    p.wide = access == 2;
     const Shape s = shape_of(d.channels, spread);
     p.tpr_log = s.tpr_log;
     const double bytes = (double)d.rows * d.channels * (ss + (r ? sb : 0) + (h ? ss : 0) + (n ? sb : 0) + (ck ? 1 : 0));
@@ -409,8 +413,10 @@ void rmsnorm_bwd(Exec &ex, const revnet_norm_desc &d, const void *dn, const void
     NormArgs p = args_of(d);
     p.x = h; p.dn = dn; p.dh = dh; p.rstd_in = rstd; p.gamma = gamma; p.dx = dx; p.dr = dr; p.dgamma = dgamma; p.partial = partial;
     p.ck = ck_view(ck, d.rows, d.channels);
-    const bool spread = d.channels % 32 || !rows_aligned(h, d.ld_stream, ss) || !rows_aligned(dh, d.ld_stream, ss) || !rows_aligned(dx, d.ld_stream, ss) ||
-                        !rows_aligned(dn, d.ld_branch, sb) || !rows_aligned(dr, d.ld_branch, sb) || !rows_aligned(gamma, 0, 4);
+    const int access = std::min({row_access(h, d.ld_stream, ss, d.channels), row_access(dh, d.ld_stream, ss, d.channels), row_access(dx, d.ld_stream, ss, d.channels),
+                                 row_access(dn, d.ld_branch, sb, d.channels), row_access(dr, d.ld_branch, sb, d.channels), row_access(gamma, 0, 4, d.channels)});
+    const bool spread = access == 0;
+    p.wide = access == 2;
     const Shape s = shape_of(d.channels, spread);
     p.tpr_log = s.tpr_log;
     const int grid = grid_of(ex.ctx, d.rows, s, bwd_per_sm(s.threads));

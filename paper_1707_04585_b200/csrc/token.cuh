@@ -19,8 +19,13 @@ static inline Checkpoint ck_view(const void *buf, int64_t rows, int channels) {
     uint8_t *b = (uint8_t *)buf;
     return Checkpoint{b, b ? b + ck_scales_at(rows, channels) : nullptr, ck_pitch(channels), (uint32_t)((rows + 63) & ~int64_t(63))};
 }
-// whether 32-byte accesses reach the rows of a tensor at p, `ld` elements of `size` bytes apart, at multiples of 16 channels (null: yes)
-static inline bool rows_aligned(const void *p, int64_t ld, int size) { return !p || (((uint64_t)(uintptr_t)p | (uint64_t)ld * size) & 31) == 0; }
+// How wide the accesses to the rows of a tensor at p can be, `ld` elements of `size` bytes apart, `channels` of them in use: 2: 32 bytes at multiples
+// of 16 channels; 1: 16 bytes; 0: rows that do not consist of 16-byte pieces on 16-byte boundaries (null: 2).
+static inline int row_access(const void *p, int64_t ld, int size, int channels) {
+    if (!p) return 2;
+    const uint64_t a = (uint64_t)(uintptr_t)p | (uint64_t)ld * size;
+    return a % 16 || channels * size % 16 ? 0 : (a % 32 ? 1 : 2);
+}
 
 // ---------------------------------------------------------------- act8.cu, norm.cu, wgrad8.cu, logprobs.cu
 // q not 0: x is int32 fixed point with that step (float32 descriptor, a null)
@@ -56,9 +61,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t byte_of(const uint8_t *p) { return *p; }
 
-// A thread's 16 channels.  Rows of whole blocks of 32 on 32-byte boundaries: 16 consecutive ones, moved by wide accesses.  Any other rows
-// (SPREAD): every 32nd of 512, the lanes of a warp side by side, so that a warp's accesses are whole lines where a thread's would be an
-// element each.  `left` is the row's length minus the thread's first channel: at most 0, none of them exists; else, unless SPREAD, all do.
+// A thread's 16 channels.  Rows of 16-byte pieces on 16-byte boundaries: 16 consecutive ones, moved by accesses of 32 (`wide`) or 16 bytes.  Any
+// other rows (SPREAD): every 32nd of 512, the lanes of a warp side by side, so that a warp's accesses are whole lines where a thread's
+// would be an element each.  `left` is the row's length minus the thread's first channel.
 constexpr int kGroup = 16;
 template <bool SPREAD> __device__ __forceinline__ int first_channel(int t) { return SPREAD ? (t & ~31) * kGroup + (t & 31) : t * kGroup; }
 template <bool SPREAD> __device__ __forceinline__ int step_of(int i) { return SPREAD ? 32 * i : i; }
@@ -69,15 +74,24 @@ __device__ __forceinline__ uint32_t bits_of(const float *p) { return __float_as_
 __device__ __forceinline__ uint32_t bits_of(const bf16 *p) { return *reinterpret_cast<const uint16_t *>(p); }
 
 // elements of p (the thread's first channel), zeros where there is none
-template <bool SPREAD, class T> __device__ __forceinline__ void load_raw(const T *p, int left, Raw16<T> &r) {
+template <bool SPREAD, class T> __device__ __forceinline__ void load_raw(const T *p, int left, bool wide, Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
     if constexpr (!SPREAD) {
+        if (left >= 16 && wide) {
 #pragma unroll
-        for (int i = 0; i < W; i += 8) {
-            uint32_t t[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-            if (left > 0) ld8(reinterpret_cast<const char *>(p) + 4 * i, t, true);
+            for (int i = 0; i < W; i += 8) {
+                uint32_t t[8];
+                ld8(reinterpret_cast<const char *>(p) + 4 * i, t, true);
 #pragma unroll
-            for (int j = 0; j < 8; j++) r.w[i + j] = t[j];
+                for (int j = 0; j < 8; j++) r.w[i + j] = t[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 4) {
+                uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                if (i * 4 / (int)sizeof(T) < left) q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
+                r.w[i] = q.x; r.w[i + 1] = q.y; r.w[i + 2] = q.z; r.w[i + 3] = q.w;
+            }
         }
     } else {
 #pragma unroll
@@ -106,10 +120,10 @@ __device__ __forceinline__ void pack(const float (&v)[16], Raw16<bf16> &r) {
 }
 __device__ __forceinline__ void put_bits(float *p, uint32_t w) { *p = __uint_as_float(w); }
 __device__ __forceinline__ void put_bits(bf16 *p, uint32_t w) { *reinterpret_cast<uint16_t *>(p) = (uint16_t)w; }
-template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, int left, const Raw16<T> &r) {
+template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, int left, bool wide, const Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
     if constexpr (!SPREAD) {
-        if (left > 0) {
+        if (left >= 16 && wide) {
 #pragma unroll
             for (int i = 0; i < W; i += 8) {
                 uint32_t t[8];
@@ -117,6 +131,11 @@ template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, 
                 for (int j = 0; j < 8; j++) t[j] = r.w[i + j];
                 st8(reinterpret_cast<char *>(p) + 4 * i, t, true);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 4)
+                if (i * 4 / (int)sizeof(T) < left)
+                    *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p) + 4 * i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
         }
     } else {
 #pragma unroll
@@ -124,15 +143,15 @@ template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, 
             if (32 * i < left) put_bits(p + 32 * i, sizeof(T) == 4 ? r.w[i * sizeof(T) / 4] : r.w[i / 2] >> (16 * (i & 1)));
     }
 }
-template <bool SPREAD, class T> __device__ __forceinline__ void load16(const T *p, int left, float (&v)[16]) {
+template <bool SPREAD, class T> __device__ __forceinline__ void load16(const T *p, int left, bool wide, float (&v)[16]) {
     Raw16<T> r;
-    load_raw<SPREAD>(p, left, r);
+    load_raw<SPREAD>(p, left, wide, r);
     unpack(r, v);
 }
-template <bool SPREAD, class T> __device__ __forceinline__ void store16(T *p, int left, const float (&v)[16]) {
+template <bool SPREAD, class T> __device__ __forceinline__ void store16(T *p, int left, bool wide, const float (&v)[16]) {
     Raw16<T> r;
     pack(v, r);
-    store_raw<SPREAD>(p, left, r);
+    store_raw<SPREAD>(p, left, wide, r);
 }
 
 // ---------------------------------------------------------------- rows on their way
@@ -148,7 +167,7 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 template <class T> constexpr int kChunks = 16 * (int)sizeof(T) / 16;
 template <class T> __device__ __forceinline__ int chunk_place(int c) { return c ^ ((c >> 3) & (kChunks<T> - 1)); }
-// p: the first of the lanes' channels, `left` of them in the row (a multiple of 32); to: the lanes' part of a stage
+// p: the first of the lanes' channels, `left` of them in the row; to: the lanes' part of a stage
 template <class T> __device__ __forceinline__ void fetch_row(uint4 *to, int lanes, int lane, const T *p, int left) {
 #pragma unroll
     for (int k = 0; k < kChunks<T>; k++) {
@@ -236,20 +255,21 @@ __device__ __forceinline__ size_t scale_index(const Checkpoint &ck, size_t row, 
 template <bool SPREAD, int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16], int end = 0) {
     if (end == 0) end = ck.pitch;
     if constexpr (SPREAD) {
-        // the lanes of a warp hold the 32 channels of a block
-        const int ch0 = ch & ~31;
+        // the lanes of a warp hold the 32 channels of a block; lane i writes the scale of block i
+        const int ch0 = ch & ~31, lane = ch & 31;
+        uint32_t mine = 0;
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             if (ch0 + 32 * i >= end) break;
             const uint32_t byte = scale_byte<CODE>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
-            if (!live) continue;
+            if (lane == i) mine = byte;
             const float inv = __uint_as_float((254u - byte) << 23);
             uint32_t c;
             if constexpr (CODE == REVNET_INT8) c = __float_as_uint(__fmaf_rn(v[i], inv, 12582912.f));
             else c = __nv_cvt_float_to_fp8(v[i] * inv, __NV_SATFINITE, __NV_E4M3);
-            ck.codes[row * ck.pitch + ch + 32 * i] = byte == 255u ? (uint8_t)0 : (uint8_t)c;
-            if ((ch & 31) == 0) ck.scales[scale_index(ck, row, ch + 32 * i)] = (uint8_t)byte;
+            if (live) ck.codes[row * ck.pitch + ch + 32 * i] = byte == 255u ? (uint8_t)0 : (uint8_t)c;
         }
+        if (live && lane < 16 && ch0 + 32 * lane < end) ck.scales[scale_index(ck, row, ch0 + 32 * lane)] = (uint8_t)mine;
     } else {
         uint32_t top = abs_max16(v);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -271,7 +291,10 @@ template <bool SPREAD> __device__ __forceinline__ void load_codes(const Checkpoi
         for (int i = 0; i < 16; i++)
             if (32 * i < left) {
                 c[i / 4] |= byte_of(ck.codes + row * ck.pitch + ch + 32 * i) << (8 * (i & 3));
-                b[i / 4] |= byte_of(ck.scales + scale_index(ck, row, ch + 32 * i)) << (8 * (i & 3));
+                // the scales of four blocks are one word where the first is a multiple of four (always but in a gated row's second half); bytes behind the
+                // last block are not used
+                if (i % 4 == 0 && (ch & 96) == 0) b[i / 4] = *reinterpret_cast<const uint32_t *>(ck.scales + scale_index(ck, row, ch + 32 * i));
+                if ((ch & 96) != 0) b[i / 4] |= byte_of(ck.scales + scale_index(ck, row, ch + 32 * i)) << (8 * (i & 3));
             }
         r.q = make_uint4(c[0], c[1], c[2], c[3]);
         r.bytes = make_uint4(b[0], b[1], b[2], b[3]);

@@ -513,7 +513,7 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
         const unsigned grid = (unsigned)(((uint64_t)rows_step * groups + 255) / 256);
         const double bytes = (double)d.rows * d.cout * (d.dy_dtype == REVNET_F32 ? 10 : 4);
         if (d.dy_dtype == REVNET_F32)
-            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<float>, grid, 256, 0, (const float *)dy, d.ld_dy, rows_aligned(dy, d.ld_dy, 4), (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
+            launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<float>, grid, 256, 0, (const float *)dy, d.ld_dy, row_access(dy, d.ld_dy, 4, 4) > 0, (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
         else
             launch_stream(ex, bytes, 0, wgrad8_prepare_kernel<bf16>, grid, 256, 0, (const bf16 *)dy, d.ld_dy, false, (bf16 *)workspace, a.rows, rows_step, d.cout, w.pitch, fast_div(groups));
         ex.check("wgrad8_prepare", bytes);
