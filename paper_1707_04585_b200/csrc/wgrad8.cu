@@ -4,12 +4,18 @@
 // (tcgen05 cta_group::2).  The values of a checkpoint are bf16 numbers, so a tile of codes becomes an MMA operand without rounding:
 //
 //   dy     TMA -> shared memory, 64 rows x 64 channels per box, 128-byte swizzle, M-major: the A operand as it lies
-//   codes  TMA -> shared memory (64 rows x 128 channels) -> eight decoder warps -> bf16 in the same swizzled layout: the B operand
+//   codes  TMA -> shared memory (64 rows x 128 channels) -> twelve decoder warps -> bf16 in the same swizzled layout: the B operand
 //   D      256 output channels x 256 input channels of fp32 in the pair's tensor memory, twice
 //
 // Long sums: the tensor cores round their running sum towards zero, an error that grows with the number of rows (7.8e-6 relative after about
-// 10000).  So a run of MMAs covers 2048 rows; the decoder warps then add its result to sums in registers (128 per thread), to nearest,
-// while the MMAs of the next run fill the other half of tensor memory.
+// 10000).  So a run of MMAs covers 2048 rows; eight warps of their own then add its result to sums in registers (128 per thread), to
+// nearest, while the MMAs of the next run fill the other half of tensor memory: 5e-7 for any number of rows.
+//
+// Decoding has to keep up with 512 clocks of MMAs per 64 x 128 codes, about 850 warp instructions.  What it took, 16384 rows, 4096 x 4096:
+// 854 us with eight warps that reported every step at cluster scope, 740 at CTA scope, 557 with steps dealt out to groups of warps so that
+// several are in flight, 415 with twelve warps of 40 registers beside the summing ones of 160, 390 in groups of two.  Without any decoding it
+// takes 301, but twelve warps that decode also draw power: 382 us (1440 TFLOP/s) in a short burst, 465 (1180) back to back at the power limit,
+// where the library's product of two bf16 matrices of this shape takes 419.
 //
 // Schedule: with P pairs resident, pair p takes the tiles p, p + P, ... as long as there is one for every pair, all of them at the same rows
 // at the same time (so that L2 serves what they share); the steps of the tiles left over are dealt out evenly, tile after tile, pair p of P'
@@ -21,7 +27,7 @@
 namespace {
 using namespace tc;
 
-constexpr int kThreads = 768;        // warp 0: dy loads, 1: MMAs, 2: codes, 3: tensor memory; 4..11: decoders, which also keep and store the sums
+constexpr int kThreads = 768;        // warp 0: dy loads, 1: MMAs, 2: codes, 3: tensor memory; 4..11: sums and stores; 12..23: decoders
 constexpr int kSummers = 8, kDecoders = 12;
 constexpr int kGroups = 6, kGroupWarps = kDecoders / kGroups;    // every kGroups-th step is decoded by the same kGroupWarps warps
 constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
@@ -64,6 +70,7 @@ struct alignas(64) Wgrad8Args {
     uint32_t rows_pad;
     int vec;                         // dW rows take stores of 16 bytes
 };
+
 // The pieces of work of a pair, in order; every role of both CTAs walks the same list.
 struct Pieces {
     const Wgrad8Args &p;
@@ -149,8 +156,9 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
     const uint32_t tmem = sh.tmem;
 
     if (warp < 4) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
-      if (warp == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    }
+    if (warp == 0) {
         const uint32_t full0 = mapa_shared(smem_u32(&sh.a_full[0]), 0);
         int s = 0; uint32_t round = 0;
         bool ok = true;
@@ -167,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
                 if (++s == kA) { s = 0; round++; }
             }
         }
-      } else if (warp == 1) {
+    } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
             const uint32_t idesc = instr_desc_m256(kN) | (3u << 15);     // both operands M / N-major
             const uint64_t da0 = smem_desc_mn(smem_u32(ring_a), 128, kBlock), db0 = smem_desc_mn(smem_u32(ring_b), 128, kBlock);
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
             }
             if (!ok) atomicExch(&sh.failed, 1u);
         }
-      } else if (warp == 2) {
+    } else if (warp == 2) {
         int s = 0; uint32_t round = 0;
         bool ok = true;
         while (ok && job.next()) {
@@ -217,8 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
                 if (++s == kC) { s = 0; round++; }
             }
         }
-      }
-    } else if (warp < 4 + kSummers) {
+    } else if (warp >= 4 && warp < 4 + kSummers) {
         // sums: a warp holds 32 of the CTA's 128 output channels (its quarter of tensor memory) x 128 of the 256 input channels
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSums));
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -281,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_consta
                 }
             }
         }
-    } else {
+    } else if (warp >= 4 + kSummers) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
         const int d = warp - 4 - kSummers;
         // a step's 64 rows x 4 blocks of 32 channels: `sub` is half a column of them (32 rows, one per lane)
