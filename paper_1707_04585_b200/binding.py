@@ -139,8 +139,13 @@ def _stream():
 
 class Context:
     def __init__(self, device: int = 0):
+        global _types
+        if not _types:
+            import torch
+            _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
         self.h = C.c_void_p()
         self.device = device
+        self.home = device if device >= 0 else -2        # where tensors have to be (a CPU tensor calls its place -1)
         rc = lib().revnet_create(C.byref(self.h), C.c_int(device))
         if rc:
             raise RevnetError(f"revnet_create failed ({rc})")
@@ -461,16 +466,8 @@ def _bad(what, name, why):
     raise e
 
 
-_types = None           # torch's types by revnet_dtype, then those of flat buffers; filled at the first call, so that importing this module needs no torch
+_types = ()             # torch's types by revnet_dtype, then those of flat buffers; filled with the first context, so that importing this module needs no torch
 F32, BF16, I32, U8 = 0, 1, 2, 3
-
-
-def _type(i):
-    global _types
-    if _types is None:
-        import torch
-        _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
-    return _types[i]
 
 
 def _strided(stride, rows, channels, ld):
@@ -481,8 +478,8 @@ def _row_ptr(ctx, what, name, t, rows, channels, ld, dtype):
     """Address of a [rows][channels] tensor (None: null)."""
     if t is None:
         return None
-    if t.dtype is not _type(dtype) or t.get_device() != ctx.device or ctx.device < 0:
-        _bad(what, name, f"must be {_type(dtype)} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if t.dtype is not _types[dtype] or t.get_device() != ctx.home:
+        _bad(what, name, f"must be {_types[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
     if t.shape != (rows, channels) or not ((ld or channels) == channels and t.is_contiguous() or _strided(t.stride(), rows, channels, ld or channels)):
         _bad(what, name, f"must be [{rows}][{channels}] with rows {ld or channels} elements apart, got shape {tuple(t.shape)}, strides {t.stride()}")
     return t.data_ptr()
@@ -492,8 +489,8 @@ def _flat_ptr(ctx, what, name, t, n, dtype=F32):
     """Address of n contiguous elements, or of at least n bytes (None: null)."""
     if t is None:
         return None
-    if t.dtype is not _type(dtype) or t.get_device() != ctx.device or ctx.device < 0 or not t.is_contiguous():
-        _bad(what, name, f"must be contiguous {_type(dtype)} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
+    if t.dtype is not _types[dtype] or t.get_device() != ctx.home or not t.is_contiguous():
+        _bad(what, name, f"must be contiguous {_types[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
     if t.numel() < n if dtype == U8 else t.numel() != n:
         _bad(what, name, f"must hold {n} elements, got {t.numel()}")
     return t.data_ptr()
@@ -511,7 +508,7 @@ def _ws(ctx, what, t):
     """Address and size of a workspace (None: null, 0)."""
     if t is None:
         return None, 0
-    if t.get_device() != ctx.device or not t.is_contiguous():
+    if t.get_device() != ctx.home or not t.is_contiguous():
         _bad(what, "workspace", f"must be contiguous on cuda:{ctx.device}, got one on {t.device}")
     return t.data_ptr(), t.numel() * t.element_size()
 
