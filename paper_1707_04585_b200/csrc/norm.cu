@@ -5,9 +5,10 @@
 //
 // HBM bounds both.  A row stays in the registers of the threads that own it, so every tensor is read and written once: the sum of squares
 // (backward: that and the sum of gamma dn h) is one reduction over the row, and everything else is local to a thread's 16 channels
-// (token.cuh).  A row belongs to `tpr` threads, a power of two: up to 32 of them reduce by shuffles, more through shared memory.  Short
-// rows share a CTA.  CTAs are resident and walk over the rows; while one row is reduced and written, the next ones are on their way into
-// shared memory (up to 8192 channels of rows in 16-byte pieces; others are loaded when they are needed).
+// (token.cuh).  A row belongs to `tpr` threads, as few as its channels take: up to 32 of them reduce by shuffles, more through shared memory.
+// Short rows share a CTA.  CTAs are resident and walk over the rows; while one row is reduced and written, the next ones are on their way into
+// shared memory (rows in 16-byte pieces, as far as two fit; others are loaded when they are needed).  With idle threads up to the next power of
+// two the warps' instructions bound rows in between: 8192 x 5120 bf16, forward 80 -> 63 us, backward 86 -> 69.
 #include "token.cuh"
 #include <algorithm>
 #include <type_traits>
@@ -22,7 +23,8 @@ struct NormArgs {
     Checkpoint ck;
     int64_t rows, ld_s, ld_b;
     int channels;
-    int tpr_log;                     // threads per row
+    int tpr;                         // threads per row
+    int stages;                      // rows of a CTA in shared memory
     int ck_scaled;
     bool wide;                       // 32-byte accesses (token.cuh)
     float eps, inv_c;
@@ -35,9 +37,9 @@ template <bool SPREAD> __device__ __forceinline__ void load_gamma(const NormArgs
     for (int i = 0; i < 16; i++) g[i] = ch + step_of<SPREAD>(i) < p.channels ? 1.f : 0.f;
 }
 
-// sums over the tpr threads of a row, given to all of them; red: N floats per warp.  Every thread of the CTA calls it.
-template <int N> __device__ __forceinline__ void row_sum(float (&v)[N], int tpr_log, float (*red)[N]) {
-    const int tpr = 1 << tpr_log;
+// sums over the tpr threads of a row, given to all of them; red: N floats per warp, the other half of them at every call, so that one barrier
+// is enough: who writes a half has passed the barrier behind its readers.  Every thread of the CTA calls it.
+template <int N, int WARPS> __device__ __forceinline__ void row_sum(float (&v)[N], int tpr, int row, int &half, float (*red)[WARPS][N]) {
 #pragma unroll
     for (int o = 16; o; o >>= 1)
         if (o < tpr) {
@@ -45,73 +47,86 @@ template <int N> __device__ __forceinline__ void row_sum(float (&v)[N], int tpr_
             for (int i = 0; i < N; i++) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
         }
     if (tpr <= 32) return;
-    const int warp = threadIdx.x >> 5, warps = tpr >> 5, first = warp & ~(warps - 1);
-    __syncthreads();                 // the last call's sums have been read
-    if ((threadIdx.x & 31) == 0) {
+    const int lane = threadIdx.x & 31, warps = tpr >> 5, first = row * warps;
+    if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < N; i++) red[warp][i] = v[i];
+        for (int i = 0; i < N; i++) red[half][threadIdx.x >> 5][i] = v[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = red[first][i];
+    for (int i = 0; i < N; i++) v[i] = lane < warps ? red[half][first + lane][i] : 0.f;
 #pragma unroll
-    for (int w = 1; w < 16; w++)
-        if (w < warps) {
+    for (int o = WARPS / 2; o; o >>= 1) {
 #pragma unroll
-            for (int i = 0; i < N; i++) v[i] += red[first + w][i];
-        }
+        for (int i = 0; i < N; i++) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+    half ^= 1;
 }
 
-// How many rows of a CTA lie in shared memory (the one that is worked on among them), and how many CTAs an SM holds, by the chunks of 16 bytes
-// that a row takes per thread.  More of either only makes the reads and writes that HBM sees at a time more scattered: forward, bf16, 16384 x 4096,
-// 2 CTAs x 2 rows 98 us, 3 x 2 101, 2 x 3 112, 4 x 3 105, 3 x 4 117; float32 stream of 200704 x 512, 3 x 2 223, 2 x 2 233, 4 x 2 263;
-// its backward pass, 2 x 2 172, 2 x 3 190.  A CTA of 512 threads is alone on its SM: 8192 x 8192, 3 rows 94, 2 103.
-__host__ __device__ constexpr int fwd_stages(int threads) { return threads == 512 ? 3 : 2; }
-__host__ __device__ constexpr int fwd_per_sm(int threads, int chunks) { return threads == 512 ? 1 : (chunks <= 4 ? 2 : 3); }
-__host__ __device__ constexpr int bwd_stages(int chunks) { return chunks <= 5 ? 3 : 2; }
-__host__ __device__ constexpr int bwd_per_sm(int threads) { return threads == 512 ? 1 : 2; }
+// How many rows of a CTA lie in shared memory (the one that is worked on among them) and how many CTAs an SM holds.  Enough bytes have to be in
+// flight, but the reads and writes that HBM sees at a time must not be scattered over too many rows.  Forward, us by CTAs x rows (KB of them per SM):
+// 16384 x 4096 bf16 1 x 2 (32) 131, 1 x 3 (48) 112, 2 x 2 (64) 99, 2 x 3 (96) 114; 200704 x 512 float32 1 x 2 (64) 281, 1 x 3 (96) 306, 2 x 2 (128) 305;
+// 8192 x 7168 float32 stream, bf16 branch 1 x 2 (84) 120, 1 x 3 (126) 137; 8192 x 6144 bf16, alone on its SM, 1 x 2 (48) 84, 1 x 3 (72) 73.
+// Backward, with more reads per write, gains from more: 16384 x 4096 bf16 2 x 2 (80) 90, 2 x 3 (120) 83, 2 x 4 (160) 84; 4096 float32 2 x 2 (144)
+// 138, 2 x 3 (216) 151; 200704 x 512 float32 from h 1 x 3 (144) 238, 2 x 2 (192) 239.  More than three rows never paid.  (With 80 registers, for three
+// CTAs, a float32 stream with a bf16 branch spills: 16384 x 4096 150 against 136.)
+constexpr int kMaxStages = 3, kFwdBytes = 96 * 1024, kBwdBytes = 160 * 1024;
+__host__ __device__ constexpr int per_sm_of(int threads) { return threads == 512 ? 1 : 2; }        // of the most threads, with 128 registers each
+__host__ __device__ constexpr int shared_of(int per_sm) { return (228 / per_sm - 2) * 1024; }        // bytes of a CTA for stages: an SM has 228 KB, the system takes 1 KB per CTA, the sums less than another
+__host__ __device__ constexpr bool staged(bool spread, int chunks) { return !spread && 2 * chunks * 16 <= shared_of(1); }      // chunks of a stage
+// the row that comes next has arrived: only the copies of the one behind it may be on their way
+__device__ __forceinline__ void next_row_wait(int stages) {
+    if (stages == 2) copies_wait<0>();
+    else copies_wait<1>();
+}
 
 // SLOTS times 16 channels per thread
 template <bool SPREAD, class TS, class TB, int CODE, int SLOTS, int THREADS>
-__global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kChunks<TB>)) rmsnorm_fwd_kernel(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kernel(const __grid_constant__ NormArgs p) {
     extern __shared__ uint4 stages[];
-    __shared__ float red[THREADS / 32][1];
-    constexpr int kX = kChunks<TS>, kPer = kX + kChunks<TB>, kStages = fwd_stages(THREADS);      // chunks: of x; of a row, r behind x
-    constexpr bool kAsync = !SPREAD && SLOTS == 1;       // (longer rows have no room for stages)
-    const int tpr = 1 << p.tpr_log, t = threadIdx.x & (tpr - 1), at_once = THREADS >> p.tpr_log;
+    __shared__ float red[2][THREADS / 32][1];
+    constexpr int kX = kChunks<TS>, kPer = kX + kChunks<TB>;      // chunks: of x; of 16 channels, r behind x
+    constexpr bool kAsync = staged(SPREAD, SLOTS * kPer * THREADS);
+    const int threads = blockDim.x, per_stage = SLOTS * kPer * threads;
+    const int tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
     const int64_t step = (int64_t)gridDim.x * at_once;
-    int64_t row = (int64_t)blockIdx.x * at_once + (threadIdx.x >> p.tpr_log);
+    int64_t row = (int64_t)blockIdx.x * at_once + which;
+    int half = 0;
     const int ch0 = first_channel<SPREAD>(t);
     float gamma[16];
     pdl_enter();
     load_gamma<SPREAD>(p, ch0, gamma);
-    // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (THREADS threads' worth)
+    // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (one per thread)
     const int lanes = tpr < 32 ? tpr : 32, lane = t & (lanes - 1), chw = (t - lane) * kGroup, mine = (int)threadIdx.x - lane;
     auto fetch = [&](int stage, int64_t at) {
-        uint4 *to = stages + stage * kPer * THREADS;
-        const int left = at < p.rows ? p.channels - chw : 0;
-        fetch_row(to + mine * kX, lanes, lane, (const TS *)p.x + (at * p.ld_s + chw), left);
-        if (p.r) fetch_row(to + kX * THREADS + mine * kChunks<TB>, lanes, lane, (const TB *)p.r + (at * p.ld_b + chw), left);
-    };
-    if constexpr (kAsync) {
 #pragma unroll
-        for (int i = 0; i < kStages - 1; i++) { fetch(i, row + i * step); copies_commit(); }
-    }
+        for (int s = 0; s < SLOTS; s++) {
+            uint4 *to = stages + stage * per_stage + s * kPer * threads;
+            const int ch = chw + s * tpr * kGroup, left = at < p.rows ? p.channels - ch : 0;
+            fetch_row(to + mine * kX, lanes, lane, (const TS *)p.x + (at * p.ld_s + ch), left);
+            if (p.r) fetch_row(to + kX * threads + mine * kChunks<TB>, lanes, lane, (const TB *)p.r + (at * p.ld_b + ch), left);
+        }
+        copies_commit();
+    };
+    if constexpr (kAsync)
+        for (int i = 0; i < p.stages - 1; i++) fetch(i, row + i * step);
     int stage = 0;
     for (int64_t row0 = (int64_t)blockIdx.x * at_once; row0 < p.rows; row0 += step, row += step) {
         const bool row_ok = row < p.rows;
         const int64_t at_s = row * p.ld_s, at_b = row * p.ld_b;
         float h[SLOTS][16], sum[1] = {0.f};
-        if constexpr (kAsync) { copies_wait<kStages - 2>(); __syncwarp(); }
-        const uint4 *from = stages + stage * kPer * THREADS;
+        if constexpr (kAsync) { next_row_wait(p.stages); __syncwarp(); }
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
             const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
             Raw16<TS> x;
             Raw16<TB> r;
             if constexpr (kAsync) {
+                const uint4 *from = stages + stage * per_stage + s * kPer * threads;
                 fetched(from + mine * kX, lane, x);
-                if (p.r) fetched(from + kX * THREADS + mine * kChunks<TB>, lane, r);
+                if (p.r) fetched(from + kX * threads + mine * kChunks<TB>, lane, r);
             } else {
                 load_raw<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x);
                 if (p.r) load_raw<SPREAD>((const TB *)p.r + (at_b + ch), left, p.wide, r);
@@ -131,11 +146,10 @@ __global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kCh
         }
         if constexpr (kAsync) {
             // into the stage that the row before this one has left
-            fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step);
-            copies_commit();
-            if (++stage == kStages) stage = 0;
+            fetch(stage == 0 ? p.stages - 1 : stage - 1, row + (p.stages - 1) * step);
+            if (++stage == p.stages) stage = 0;
         }
-        row_sum(sum, p.tpr_log, red);
+        row_sum(sum, tpr, which, half, red);
         const float rstd = rsqrtf(sum[0] * p.inv_c + p.eps);
         if (p.rstd && row_ok && t == 0) p.rstd[row] = rstd;
         if (!p.n && !p.ck.codes) continue;
@@ -159,15 +173,18 @@ __global__ void __launch_bounds__(THREADS, fwd_per_sm(THREADS, kChunks<TS> + kCh
 
 // FROM_H: from h; else from a checkpoint of xh with CODE.  A thread keeps its channels for all rows it works on, and their dgamma in registers.
 template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS>
-__global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kernel(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kernel(const __grid_constant__ NormArgs p) {
     extern __shared__ uint4 stages[];
     constexpr int kSums = FROM_H ? 2 : 1;                // gamma dn x, and the squares
-    __shared__ float red[THREADS / 32][kSums];
-    constexpr int kS = kChunks<TS>, kB = kChunks<TB>, kX = FROM_H ? kS : 1, kPer = kS + kB + kX, kStages = bwd_stages(kPer);      // chunks of a row: dh, dn, h or codes
-    constexpr bool kAsync = !SPREAD && SLOTS == 1;       // (longer rows have no room for stages)
-    const int tpr = 1 << p.tpr_log, t = threadIdx.x & (tpr - 1), at_once = THREADS >> p.tpr_log;
+    __shared__ float red[2][THREADS / 32][kSums];
+    constexpr int kS = kChunks<TS>, kB = kChunks<TB>, kX = FROM_H ? kS : 1, kPer = kS + kB + kX;      // chunks of 16 channels: dh, dn, h or codes
+    constexpr bool kAsync = staged(SPREAD, SLOTS * kPer * THREADS);
+    constexpr bool kAgain = kAsync && SLOTS > 1;         // longer rows are decoded a second time: their registers hold dgamma
+    const int threads = blockDim.x, per_stage = SLOTS * kPer * threads;
+    const int tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
     const int64_t step = (int64_t)gridDim.x * at_once;
-    int64_t row = (int64_t)blockIdx.x * at_once + (threadIdx.x >> p.tpr_log);
+    int64_t row = (int64_t)blockIdx.x * at_once + which;
+    int half = 0;
     const int ch0 = first_channel<SPREAD>(t);
     float dg[SLOTS][16], gamma[16];
 #pragma unroll
@@ -176,76 +193,89 @@ __global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kern
         for (int i = 0; i < 16; i++) dg[s][i] = 0.f;
     pdl_enter();
     load_gamma<SPREAD>(p, ch0, gamma);
-    // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (THREADS threads' worth)
+    // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (one per thread)
     const int lanes = tpr < 32 ? tpr : 32, lane = t & (lanes - 1), chw = (t - lane) * kGroup, mine = (int)threadIdx.x - lane;
     auto fetch = [&](int stage, int64_t at) {
-        uint4 *to = stages + stage * kPer * THREADS;
-        const int left = at < p.rows ? p.channels - chw : 0;
-        if (p.dh) fetch_row(to + mine * kS, lanes, lane, (const TS *)p.dh + (at * p.ld_s + chw), left);
-        fetch_row(to + kS * THREADS + mine * kB, lanes, lane, (const TB *)p.dn + (at * p.ld_b + chw), left);
-        if constexpr (FROM_H) fetch_row(to + (kS + kB) * THREADS + mine * kS, lanes, lane, (const TS *)p.x + (at * p.ld_s + chw), left);
-        else copy16(to + (kS + kB) * THREADS + threadIdx.x, p.ck.codes + (at * p.ck.pitch + ch0), lane * kGroup < left);
-    };
-    if constexpr (kAsync) {
 #pragma unroll
-        for (int i = 0; i < kStages - 1; i++) { fetch(i, row + i * step); copies_commit(); }
-    }
+        for (int s = 0; s < SLOTS; s++) {
+            uint4 *to = stages + stage * per_stage + s * kPer * threads;
+            const int ch = chw + s * tpr * kGroup, left = at < p.rows ? p.channels - ch : 0;
+            if (p.dh) fetch_row(to + mine * kS, lanes, lane, (const TS *)p.dh + (at * p.ld_s + ch), left);
+            fetch_row(to + kS * threads + mine * kB, lanes, lane, (const TB *)p.dn + (at * p.ld_b + ch), left);
+            if constexpr (FROM_H) fetch_row(to + (kS + kB) * threads + mine * kS, lanes, lane, (const TS *)p.x + (at * p.ld_s + ch), left);
+            else copy16(to + (kS + kB) * threads + threadIdx.x, p.ck.codes + (at * p.ck.pitch + ch + lane * kGroup), lane * kGroup < left);
+        }
+        copies_commit();
+    };
+    if constexpr (kAsync)
+        for (int i = 0; i < p.stages - 1; i++) fetch(i, row + i * step);
     int stage = 0;
     // what a row has besides its channels is loaded a row ahead too
     float rstd_next = 0.f;
-    uint32_t byte_next = 0;
+    uint32_t byte_next[SLOTS] = {}, bytes[SLOTS];
     auto ahead = [&](int64_t at) {
         if (FROM_H) return;
         rstd_next = at < p.rows ? p.rstd_in[at] : 0.f;
-        if (kAsync) byte_next = at < p.rows && ch0 < p.channels ? byte_of(p.ck.scales + scale_index(p.ck, at, ch0)) : 0u;
+        if (kAsync) {
+#pragma unroll
+            for (int s = 0; s < SLOTS; s++) {
+                const int ch = ch0 + s * tpr * kGroup;
+                byte_next[s] = at < p.rows && ch < p.channels ? byte_of(p.ck.scales + scale_index(p.ck, at, ch)) : 0u;
+            }
+        }
+    };
+    // what the sums and dx need of slot s, out of a stage
+    auto staged_row = [&](int stage, int s, float (&x)[16], float (&dn)[16]) {
+        const uint4 *from = stages + stage * per_stage + s * kPer * threads;
+        Raw16<TB> rn;
+        fetched(from + kS * threads + mine * kB, lane, rn);
+        unpack(rn, dn);
+        if constexpr (FROM_H) {
+            Raw16<TS> rx;
+            fetched(from + (kS + kB) * threads + mine * kS, lane, rx);
+            unpack(rx, x);
+        } else decode16<CODE>(from[(kS + kB) * threads + threadIdx.x], bytes[s], x);
     };
     ahead(row);
     for (int64_t row0 = (int64_t)blockIdx.x * at_once; row0 < p.rows; row0 += step, row += step) {
         const bool row_ok = row < p.rows;
         const int64_t at_s = row * p.ld_s, at_b = row * p.ld_b;
-        float x[SLOTS][16], dn[SLOTS][16], rstd = rstd_next, sum[kSums];
+        constexpr int kHeld = kAgain ? 1 : SLOTS;
+        float x[kHeld][16], dn[kHeld][16], rstd = rstd_next, sum[kSums];
+#pragma unroll
+        for (int s = 0; s < SLOTS; s++) bytes[s] = byte_next[s];
 #pragma unroll
         for (int i = 0; i < kSums; i++) sum[i] = 0.f;
-        if constexpr (kAsync) { copies_wait<kStages - 2>(); __syncwarp(); }
-        const uint4 *from = stages + stage * kPer * THREADS;
+        if constexpr (kAsync) { next_row_wait(p.stages); __syncwarp(); }
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
             const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
-            if constexpr (kAsync) {
-                Raw16<TB> rn;
-                fetched(from + kS * THREADS + mine * kB, lane, rn);
-                unpack(rn, dn[s]);
-                if constexpr (FROM_H) {
-                    Raw16<TS> rx;
-                    fetched(from + (kS + kB) * THREADS + mine * kS, lane, rx);
-                    unpack(rx, x[s]);
-                } else decode16<CODE>(from[(kS + kB) * THREADS + threadIdx.x], byte_next, x[s]);
-            } else {
-                load16<SPREAD>((const TB *)p.dn + (at_b + ch), left, p.wide, dn[s]);
-                if constexpr (FROM_H) load16<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x[s]);
-                else read16<SPREAD, CODE>(p.ck, row, ch, left, x[s]);
-                if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
+            const int k = kAgain ? 0 : s;
+            if constexpr (kAsync) staged_row(stage, s, x[k], dn[k]);
+            else {
+                load16<SPREAD>((const TB *)p.dn + (at_b + ch), left, p.wide, dn[k]);
+                if constexpr (FROM_H) load16<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x[k]);
+                else read16<SPREAD, CODE>(p.ck, row, ch, left, x[k]);
             }
+            if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 if constexpr (FROM_H) {
-                    sum[0] = fmaf(dn[s][i] * gamma[i], x[s][i], sum[0]);
-                    sum[1] = fmaf(x[s][i], x[s][i], sum[1]);
+                    sum[0] = fmaf(dn[k][i] * gamma[i], x[k][i], sum[0]);
+                    sum[1] = fmaf(x[k][i], x[k][i], sum[1]);
                 } else {
-                    dg[s][i] = fmaf(dn[s][i], x[s][i], dg[s][i]);         // (zeros where there is no row)
-                    dn[s][i] *= gamma[i];
-                    sum[0] = fmaf(dn[s][i], x[s][i], sum[0]);
+                    dg[s][i] = fmaf(dn[k][i], x[k][i], dg[s][i]);         // (zeros where there is no row)
+                    dn[k][i] *= gamma[i];
+                    sum[0] = fmaf(dn[k][i], x[k][i], sum[0]);
                 }
             }
         }
         ahead(row + step);
         if constexpr (kAsync) {
             // into the stage that the row before this one has left
-            fetch(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * step);
-            copies_commit();
-            if (++stage == kStages) stage = 0;
+            fetch(stage == 0 ? p.stages - 1 : stage - 1, row + (p.stages - 1) * step);
         }
-        row_sum(sum, p.tpr_log, red);
+        row_sum(sum, tpr, which, half, red);
         if constexpr (FROM_H) rstd = rsqrtf(sum[1] * p.inv_c + p.eps);
         // dx = dh + rstd gamma dn - xh (rstd mean(gamma dn xh)); from h: xh = h rstd, and the mean is rstd times that of gamma dn h
         const float back = -sum[0] * p.inv_c * rstd * (FROM_H ? rstd * rstd : 1.f);
@@ -255,41 +285,42 @@ __global__ void __launch_bounds__(THREADS, bwd_per_sm(THREADS)) rmsnorm_bwd_kern
             float d[16];
             if (p.dh) {
                 Raw16<TS> rh;
-                if constexpr (kAsync) fetched(from + mine * kS, lane, rh);
+                if constexpr (kAsync) fetched(stages + stage * per_stage + s * kPer * threads + mine * kS, lane, rh);
                 else load_raw<SPREAD>((const TS *)p.dh + (at_s + ch), left, p.wide, rh);
                 unpack(rh, d);
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; i++) d[i] = 0.f;
             }
-            if (SLOTS > 1 && FROM_H) load_gamma<SPREAD>(p, ch, gamma);
+            const int k = kAgain ? 0 : s;
+            if (SLOTS > 1 && (FROM_H || kAgain)) load_gamma<SPREAD>(p, ch, gamma);
+            if constexpr (kAgain) staged_row(stage, s, x[0], dn[0]);
 #pragma unroll
             for (int i = 0; i < 16; i++) {
-                float w = dn[s][i] * rstd;
-                if constexpr (FROM_H) {
-                    dg[s][i] = fmaf(w, x[s][i], dg[s][i]);
-                    w *= gamma[i];
-                }
-                d[i] = fmaf(x[s][i], back, d[i] + w);
+                float w = dn[k][i] * rstd;
+                if constexpr (FROM_H) dg[s][i] = fmaf(w, x[k][i], dg[s][i]);
+                if constexpr (FROM_H || kAgain) w *= gamma[i];
+                d[i] = fmaf(x[k][i], back, d[i] + w);
             }
             store16<SPREAD>((TS *)p.dx + (at_s + ch), left, p.wide, d);
             if (p.dr) store16<SPREAD>((TB *)p.dr + (at_b + ch), left, p.wide, d);
         }
         if (SLOTS > 1) load_gamma<SPREAD>(p, ch0, gamma);
+        if constexpr (kAsync) { if (++stage == p.stages) stage = 0; }
     }
     if constexpr (kAsync) copies_wait<0>();
     if (!p.dgamma) return;
     float *out = gridDim.x == 1 ? p.dgamma : p.partial + (size_t)blockIdx.x * p.channels;
-    if (THREADS == 256 && at_once > 1) {
+    if (SLOTS == 1 && at_once > 1) {
         // the CTA's rows first, in a fixed order, through the stages' memory
         float *sums = reinterpret_cast<float *>(stages);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 16; i++) sums[(threadIdx.x - t) * 16 + ch0 + step_of<SPREAD>(i)] = dg[0][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < p.channels; c += THREADS) {
+        for (int c = threadIdx.x; c < p.channels; c += threads) {
             float v = 0.f;
-            for (int k = 0; k < at_once; k++) v += sums[(k << p.tpr_log) * 16 + c];
+            for (int k = 0; k < at_once; k++) v += sums[k * tpr * 16 + c];
             out[c] = v;
         }
         return;
@@ -317,20 +348,34 @@ __global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float *parti
     if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + k0 < channels) dgamma[blockIdx.x * 32 + k0] = v;
 }
 
-// 16-channel groups of a row -> threads per row (log2), groups per thread and threads per CTA
-struct Shape { int tpr_log, slots, threads; };
+// 16-channel groups of a row -> threads per row (a power of two, or whole warps), groups per thread, threads per CTA, and the most of them
+struct Shape { int tpr, slots, threads, most; };
 Shape shape_of(int channels, bool spread) {
     const int groups = ck_pitch(channels) / kGroup;
-    Shape s{spread ? 5 : 1, 1, groups > 256 ? 512 : 256};       // at least the two lanes of a block of 32, or a warp
-    while ((1 << s.tpr_log) < groups && (1 << s.tpr_log) < s.threads) s.tpr_log++;
-    while ((s.slots << s.tpr_log) < groups) s.slots *= 2;
+    Shape s{spread ? 32 : 2, groups > 512 ? 2 : 1, 0, groups > 256 ? 512 : 256};       // at least the two lanes of a block of 32, or a warp
+    const int need = (groups + s.slots - 1) / s.slots;
+    while (s.tpr < need && s.tpr < 32) s.tpr *= 2;
+    if (s.tpr < need) s.tpr = (need + 31) / 32 * 32;
+    s.threads = s.most / s.tpr * s.tpr;
     return s;
 }
 // resident CTAs, no more than there are rows for
 int grid_of(const revnet_ctx *ctx, int64_t rows, const Shape &s, int per_sm) {
-    const int64_t at_once = s.threads >> s.tpr_log, need = (rows + at_once - 1) / at_once, most = (int64_t)ctx->sm_count * per_sm;
+    const int64_t at_once = s.threads / s.tpr, need = (rows + at_once - 1) / at_once, most = (int64_t)ctx->sm_count * per_sm;
     return (int)(need < most ? need : most);
 }
+// CTAs per SM and the stages of each, for rows that take `row` chunks per thread: as many CTAs as threads fit (`full` of the most threads), then
+// up to kMaxStages stages, as long as the rows in them stay within `bytes` per SM.
+struct Plan { int per_sm, stages; };
+Plan plan_of(const Shape &s, int channels, int row, int full, int bytes) {
+    const int used = s.threads / s.tpr * ((channels + kGroup - 1) / kGroup) * row * 16, stage = s.threads * s.slots * row * 16;
+    Plan p{full * s.most / s.threads, 2};
+    while (p.per_sm > 1 && (p.per_sm * 2 * used > bytes || 2 * stage > shared_of(p.per_sm))) p.per_sm--;
+    while (p.stages < kMaxStages && p.per_sm * (p.stages + 1) * used <= bytes && (p.stages + 1) * stage <= shared_of(p.per_sm)) p.stages++;
+    return p;
+}
+Plan fwd_plan(const Shape &s, int channels, int row) { return plan_of(s, channels, row, per_sm_of(s.most), s.most == 512 ? kFwdBytes : kFwdBytes - 1); }
+Plan bwd_plan(const Shape &s, int channels, int row) { return plan_of(s, channels, row, per_sm_of(s.most), kBwdBytes); }
 template <class K> bool with_shared(Exec &ex, OncePerDevice &once, K kernel, size_t bytes) {
     if (!once.first(ex.ctx->device)) return true;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
@@ -338,34 +383,36 @@ template <class K> bool with_shared(Exec &ex, OncePerDevice &once, K kernel, siz
 // records of dgamma: by the larger grid of the two forms, whose choice also depends on addresses
 int parts_of(const revnet_ctx *ctx, const revnet_norm_desc &d) {
     const Shape a = shape_of(d.channels, false), b = shape_of(d.channels, true);
-    const int ga = grid_of(ctx, d.rows, a, bwd_per_sm(a.threads)), gb = grid_of(ctx, d.rows, b, bwd_per_sm(b.threads));
+    const int ga = grid_of(ctx, d.rows, a, bwd_plan(a, d.channels, 1).per_sm), gb = grid_of(ctx, d.rows, b, bwd_plan(b, d.channels, 1).per_sm);
     return ga > gb ? ga : gb;
 }
 
-template <bool SPREAD, class TS, class TB, int CODE, int SLOTS, int THREADS> void fwd_k(Exec &ex, const NormArgs &p, unsigned grid, double bytes) {
+template <bool SPREAD, class TS, class TB, int CODE, int SLOTS, int THREADS> void fwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
     static OncePerDevice once;
-    constexpr int chunks = kChunks<TS> + kChunks<TB>;
-    const size_t smem = SPREAD || SLOTS > 1 ? 0 : (size_t)fwd_stages(THREADS) * chunks * THREADS * 16;
-    if (!with_shared(ex, once, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, smem)) return;
-    launch_stream(ex, bytes, smem ? 100 : 0, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, grid, THREADS, smem, p);
+    constexpr int row = kChunks<TS> + kChunks<TB>;
+    constexpr bool async = staged(SPREAD, SLOTS * row * THREADS);
+    p.stages = fwd_plan(s, p.channels, row).stages;
+    if (!with_shared(ex, once, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, async ? shared_of(1) : 0)) return;
+    launch_stream(ex, bytes, async ? 100 : 0, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, grid, s.threads, async ? (size_t)p.stages * s.threads * SLOTS * row * 16 : 0, p);
 }
 template <bool SPREAD, class TS, class TB, int CODE> void fwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
-    if (s.slots == 2) fwd_k<SPREAD, TS, TB, CODE, 2, 512>(ex, p, grid, bytes);
-    else if (s.threads == 512) fwd_k<SPREAD, TS, TB, CODE, 1, 512>(ex, p, grid, bytes);
-    else fwd_k<SPREAD, TS, TB, CODE, 1, 256>(ex, p, grid, bytes);
+    if (s.slots == 2) fwd_k<SPREAD, TS, TB, CODE, 2, 512>(ex, p, s, grid, bytes);
+    else if (s.most == 512) fwd_k<SPREAD, TS, TB, CODE, 1, 512>(ex, p, s, grid, bytes);
+    else fwd_k<SPREAD, TS, TB, CODE, 1, 256>(ex, p, s, grid, bytes);
 }
-template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS> void bwd_k(Exec &ex, const NormArgs &p, unsigned grid, double bytes) {
+template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS> void bwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
     static OncePerDevice once;
-    constexpr int chunks = kChunks<TS> + kChunks<TB> + (FROM_H ? kChunks<TS> : 1);
-    const size_t rows = SPREAD || SLOTS > 1 ? 0 : (size_t)bwd_stages(chunks) * chunks * THREADS * 16;
-    const size_t least = THREADS == 256 ? THREADS * 16 * sizeof(float) : 0, smem = rows > least ? rows : least;
-    if (!with_shared(ex, once, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, smem)) return;
-    launch_stream(ex, bytes, SPREAD || SLOTS > 1 ? 15 : 100, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, grid, THREADS, smem, p);
+    constexpr int row = kChunks<TS> + kChunks<TB> + (FROM_H ? kChunks<TS> : 1);
+    constexpr bool async = staged(SPREAD, SLOTS * row * THREADS);
+    p.stages = bwd_plan(s, p.channels, row).stages;
+    const size_t rows = async ? (size_t)p.stages * s.threads * SLOTS * row * 16 : 0, least = THREADS == 256 ? THREADS * 16 * sizeof(float) : 0, smem = rows > least ? rows : least;
+    if (!with_shared(ex, once, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, async ? shared_of(1) : least)) return;
+    launch_stream(ex, bytes, async ? 100 : 15, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, grid, s.threads, smem, p);
 }
 template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE> void bwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
-    if (s.slots == 2) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 2, 512>(ex, p, grid, bytes);
-    else if (s.threads == 512) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 512>(ex, p, grid, bytes);
-    else bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 256>(ex, p, grid, bytes);
+    if (s.slots == 2) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 2, 512>(ex, p, s, grid, bytes);
+    else if (s.most == 512) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 512>(ex, p, s, grid, bytes);
+    else bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 256>(ex, p, s, grid, bytes);
 }
 template <class F> void by_types(const revnet_norm_desc &d, bool spread, F &&f) {
     auto types = [&](auto s) {
@@ -395,9 +442,9 @@ void rmsnorm_fwd(Exec &ex, const revnet_norm_desc &d, const void *x, const void 
     const bool spread = access == 0;
     p.wide = access == 2;
     const Shape s = shape_of(d.channels, spread);
-    p.tpr_log = s.tpr_log;
+    p.tpr = s.tpr;
     const double bytes = (double)d.rows * d.channels * (ss + (r ? sb : 0) + (h ? ss : 0) + (n ? sb : 0) + (ck ? 1 : 0));
-    const unsigned grid = (unsigned)grid_of(ex.ctx, d.rows, s, fwd_per_sm(s.threads, ss + sb));
+    const unsigned grid = (unsigned)grid_of(ex.ctx, d.rows, s, fwd_plan(s, d.channels, ss + sb).per_sm);
     by_types(d, spread, [&](auto sp, auto ts, auto tb) {
         if (d.code == REVNET_INT8) fwd_t<decltype(sp)::value, decltype(ts), decltype(tb), REVNET_INT8>(ex, p, s, grid, bytes);
         else fwd_t<decltype(sp)::value, decltype(ts), decltype(tb), REVNET_E4M3>(ex, p, s, grid, bytes);
@@ -418,8 +465,8 @@ void rmsnorm_bwd(Exec &ex, const revnet_norm_desc &d, const void *dn, const void
     const bool spread = access == 0;
     p.wide = access == 2;
     const Shape s = shape_of(d.channels, spread);
-    p.tpr_log = s.tpr_log;
-    const int grid = grid_of(ex.ctx, d.rows, s, bwd_per_sm(s.threads));
+    p.tpr = s.tpr;
+    const int grid = grid_of(ex.ctx, d.rows, s, bwd_plan(s, d.channels, h ? ss + sb + ss : ss + sb + 1).per_sm);
     if (grid > 0) {
         const double bytes = (double)d.rows * d.channels * (sb + (dh ? ss : 0) + (h ? ss : 1) + ss + (dr ? sb : 0));
         by_types(d, spread, [&](auto sp, auto ts, auto tb) {

@@ -277,6 +277,16 @@ def test_norm_backward(ctx, rows, channels, pad, skip, stream, branch, source):
     B.revnet_rmsnorm_bwd(ctx, d, rdn.t, rdh2.t, *args, dx2.t, None, dg2, ws)
     assert torch.equal(dg, dg2) and torch.equal(dx2.t, dx.t)
 
+@pytest.mark.parametrize("rows,channels,pad", [(1300, 768, 0), (1300, 1280, 8), (700, 1504, 0), (1000, 2560, 8), (500, 4128, 0), (500, 5120, 0), (400, 8224, 8), (400, 12320, 0), (330, 16384, 0),
+                                               (500, 1283, 3), (400, 2501, 3), (330, 5001, 3), (300, 8201, 3)])
+@pytest.mark.parametrize("stream,branch", PAIRS)
+def test_norm_over_many_rows(ctx, rows, channels, pad, stream, branch):
+    """Threads per row, CTAs per SM and rows in shared memory go by the width; here every CTA works on several rows."""
+    test_norm_forward(ctx, rows, channels, pad, 0, stream, branch, "e4m3")
+    test_norm_backward(ctx, rows, channels, pad, 0, stream, branch, "int8")
+    test_norm_backward(ctx, rows, channels, pad, 0, stream, branch, "h")
+
+
 
 # ------------------------------------------------------------------ weight gradient
 def wgrad(ctx, dy, ck, cin, gamma, code, dtype):
