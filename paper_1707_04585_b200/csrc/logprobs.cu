@@ -216,12 +216,12 @@ __global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) 
     float bar = -INFINITY;           // the bound as a logit, and the largest index that still reaches it
     unsigned bar_index = 0xffffffffu;
     bool started = false;
-    if ((int)threadIdx.x < vecs) load_raw<false>(xb + head + (int)threadIdx.x * kVec, kVec, true, next);
+    if ((int)threadIdx.x < vecs) load_raw<kPieces>(xb + head + (int)threadIdx.x * kVec, 0, kVec, true, next);
     for (int v0 = warp * 32; v0 < vecs; v0 += blockDim.x) {
         const int v = v0 + lane;
         const bool ok = v < vecs;
         raw = next;
-        if (v + (int)blockDim.x < vecs) load_raw<false>(xb + head + (v + (int)blockDim.x) * kVec, kVec, true, next);
+        if (v + (int)blockDim.x < vecs) load_raw<kPieces>(xb + head + (v + (int)blockDim.x) * kVec, 0, kVec, true, next);
         float f[kVec];
         const float top = top_of(raw);
         unpack(raw, f);
@@ -364,14 +364,14 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogpArgs p) {
     const int vecs = (len - head) / kVec, tail0 = head + vecs * kVec;
     for (int v = threadIdx.x; v < vecs; v += blockDim.x) {
         float f[kVec];
-        load16<false>(x + head + v * kVec, kVec, true, f);
+        load16<kPieces>(x + head + v * kVec, 0, kVec, true, f);
         const int at = tgt - (begin + head + v * kVec);
 #pragma unroll
         for (int i = 0; i < kVec; i++) {
             const float d = none ? 0.f : grad(f[i], lse, g, ge, ent2);
             f[i] = at == i && !none ? d + g : d;
         }
-        store16<false>(dx + head + v * kVec, kVec, true, f);
+        store16<kPieces>(dx + head + v * kVec, 0, kVec, true, f);
     }
     for (int e = threadIdx.x; e < head + len - tail0; e += blockDim.x) {
         const int i = e < head ? e : tail0 + e - head;

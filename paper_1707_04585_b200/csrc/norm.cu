@@ -31,10 +31,10 @@ struct NormArgs {
 };
 
 // gamma of a thread's channels (ones where there is none, zeros behind the row's end)
-template <bool SPREAD> __device__ __forceinline__ void load_gamma(const NormArgs &p, int ch, float (&g)[16]) {
-    if (p.gamma) { load16<SPREAD>(p.gamma + ch, p.channels - ch, p.wide, g); return; }
+template <int ROWS> __device__ __forceinline__ void load_gamma(const NormArgs &p, int ch, float (&g)[16]) {
+    if (p.gamma) { load16<ROWS>(p.gamma + ch, ch, p.channels - ch, p.wide, g); return; }
 #pragma unroll
-    for (int i = 0; i < 16; i++) g[i] = ch + step_of<SPREAD>(i) < p.channels ? 1.f : 0.f;
+    for (int i = 0; i < 16; i++) g[i] = ch + i < p.channels ? 1.f : 0.f;
 }
 
 // sums over the tpr threads of a row, given to all of them; red: N floats per warp, the other half of them at every call, so that one barrier
@@ -75,7 +75,9 @@ template <int N, int WARPS> __device__ __forceinline__ void row_sum(float (&v)[N
 constexpr int kMaxStages = 3, kFwdBytes = 96 * 1024, kBwdBytes = 160 * 1024;
 __host__ __device__ constexpr int per_sm_of(int threads) { return threads == 512 ? 1 : 2; }        // of the most threads, with 128 registers each
 __host__ __device__ constexpr int shared_of(int per_sm) { return (228 / per_sm - 2) * 1024; }        // bytes of a CTA for stages: an SM has 228 KB, the system takes 1 KB per CTA, the sums less than another
-__host__ __device__ constexpr bool staged(bool spread, int chunks) { return !spread && 2 * chunks * 16 <= shared_of(1); }      // chunks of a stage
+__host__ __device__ constexpr bool staged(int rows, int slots, int row, int threads) {        // do two stages fit
+    return 2 * slots * (row * threads + (rows == kShifted ? 3 * threads / 32 : 0)) * 16 <= shared_of(1);
+}
 // the row that comes next has arrived: only the copies of the one behind it may be on their way
 __device__ __forceinline__ void next_row_wait(int stages) {
     if (stages == 2) copies_wait<0>();
@@ -83,30 +85,32 @@ __device__ __forceinline__ void next_row_wait(int stages) {
 }
 
 // SLOTS times 16 channels per thread
-template <bool SPREAD, class TS, class TB, int CODE, int SLOTS, int THREADS>
+template <int ROWS, class TS, class TB, int CODE, int SLOTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kernel(const __grid_constant__ NormArgs p) {
     extern __shared__ uint4 stages[];
     __shared__ float red[2][THREADS / 32][1];
     constexpr int kX = kChunks<TS>, kPer = kX + kChunks<TB>;      // chunks: of x; of 16 channels, r behind x
-    constexpr bool kAsync = staged(SPREAD, SLOTS * kPer * THREADS);
-    const int threads = blockDim.x, per_stage = SLOTS * kPer * threads;
-    const int tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
+    constexpr bool kAsync = staged(ROWS, SLOTS, kPer, THREADS);
+    const int threads = blockDim.x, tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
     const int64_t step = (int64_t)gridDim.x * at_once;
     int64_t row = (int64_t)blockIdx.x * at_once + which;
     int half = 0;
-    const int ch0 = first_channel<SPREAD>(t);
+    const int ch0 = t * kGroup;
     float gamma[16];
     pdl_enter();
-    load_gamma<SPREAD>(p, ch0, gamma);
+    load_gamma<ROWS>(p, ch0, gamma);
     // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (one per thread)
     const int lanes = tpr < 32 ? tpr : 32, lane = t & (lanes - 1), chw = (t - lane) * kGroup, mine = (int)threadIdx.x - lane;
+    // shifted rows have a chunk more per row and warp, in each part of a stage
+    const int extra = ROWS == kShifted ? mine / lanes : 0, extras = ROWS == kShifted ? threads / lanes : 0;
+    const int per_slot = kPer * threads + 3 * extras, per_stage = SLOTS * per_slot;
     auto fetch = [&](int stage, int64_t at) {
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            uint4 *to = stages + stage * per_stage + s * kPer * threads;
+            uint4 *to = stages + stage * per_stage + s * per_slot;
             const int ch = chw + s * tpr * kGroup, left = at < p.rows ? p.channels - ch : 0;
-            fetch_row(to + mine * kX, lanes, lane, (const TS *)p.x + (at * p.ld_s + ch), left);
-            if (p.r) fetch_row(to + kX * threads + mine * kChunks<TB>, lanes, lane, (const TB *)p.r + (at * p.ld_b + ch), left);
+            fetch_row<ROWS>(to + mine * kX + extra, lanes, lane, (const TS *)p.x, at * p.ld_s + ch, left);
+            if (p.r) fetch_row<ROWS>(to + kX * threads + extras + mine * kChunks<TB> + extra, lanes, lane, (const TB *)p.r, at * p.ld_b + ch, left);
         }
         copies_commit();
     };
@@ -120,16 +124,16 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kerne
         if constexpr (kAsync) { next_row_wait(p.stages); __syncwarp(); }
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
+            const int ch = (s * tpr + t) * kGroup, left = row_ok ? p.channels - ch : 0;
             Raw16<TS> x;
             Raw16<TB> r;
             if constexpr (kAsync) {
-                const uint4 *from = stages + stage * per_stage + s * kPer * threads;
-                fetched(from + mine * kX, lane, x);
-                if (p.r) fetched(from + kX * threads + mine * kChunks<TB>, lane, r);
+                const uint4 *from = stages + stage * per_stage + s * per_slot;
+                fetched<ROWS>(from + mine * kX + extra, lanes, lane, (const TS *)p.x + at_s, x);
+                if (p.r) fetched<ROWS>(from + kX * threads + extras + mine * kChunks<TB> + extra, lanes, lane, (const TB *)p.r + at_b, r);
             } else {
-                load_raw<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x);
-                if (p.r) load_raw<SPREAD>((const TB *)p.r + (at_b + ch), left, p.wide, r);
+                load_raw<ROWS>((const TS *)p.x + (at_s + ch), ch, left, p.wide, x);
+                if (p.r) load_raw<ROWS>((const TB *)p.r + (at_b + ch), ch, left, p.wide, r);
             }
             unpack(x, h[s]);
             if (p.r) {
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kerne
                 for (int i = 0; i < 16; i++) h[s][i] += add[i];
                 pack(h[s], x);                       // the norm is of h as it is stored, so that the backward pass sees the same h
                 unpack(x, h[s]);
-                if (p.h) store_raw<SPREAD>((TS *)p.h + (at_s + ch), left, p.wide, x);
+                if (p.h) store_raw<ROWS>((TS *)p.h + (at_s + ch), ch, left, p.wide, x);
             }
 #pragma unroll
             for (int i = 0; i < 16; i++) sum[0] = fmaf(h[s][i], h[s][i], sum[0]);
@@ -155,55 +159,57 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kerne
         if (!p.n && !p.ck.codes) continue;
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
+            const int ch = (s * tpr + t) * kGroup, left = row_ok ? p.channels - ch : 0;
             float n[16];
-            if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
+            if (s > 0) load_gamma<ROWS>(p, ch, gamma);
 #pragma unroll
             for (int i = 0; i < 16; i++) { h[s][i] *= rstd; n[i] = h[s][i] * gamma[i]; }
-            if (p.n) store16<SPREAD>((TB *)p.n + (at_b + ch), left, p.wide, n);
+            if (p.n) store16<ROWS>((TB *)p.n + (at_b + ch), ch, left, p.wide, n);
             if (p.ck.codes) {
-                if (p.ck_scaled) keep16<SPREAD, CODE>(p.ck, row, ch, row_ok, n);
-                else keep16<SPREAD, CODE>(p.ck, row, ch, row_ok, h[s]);
+                if (p.ck_scaled) keep16<CODE>(p.ck, row, ch, row_ok, n);
+                else keep16<CODE>(p.ck, row, ch, row_ok, h[s]);
             }
         }
-        if (SLOTS > 1) load_gamma<SPREAD>(p, ch0, gamma);
+        if (SLOTS > 1) load_gamma<ROWS>(p, ch0, gamma);
     }
     if constexpr (kAsync) copies_wait<0>();
 }
 
 // FROM_H: from h; else from a checkpoint of xh with CODE.  A thread keeps its channels for all rows it works on, and their dgamma in registers.
-template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS>
+template <int ROWS, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS>
 __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kernel(const __grid_constant__ NormArgs p) {
     extern __shared__ uint4 stages[];
     constexpr int kSums = FROM_H ? 2 : 1;                // gamma dn x, and the squares
     __shared__ float red[2][THREADS / 32][kSums];
     constexpr int kS = kChunks<TS>, kB = kChunks<TB>, kX = FROM_H ? kS : 1, kPer = kS + kB + kX;      // chunks of 16 channels: dh, dn, h or codes
-    constexpr bool kAsync = staged(SPREAD, SLOTS * kPer * THREADS);
+    constexpr bool kAsync = staged(ROWS, SLOTS, kPer, THREADS);
     constexpr bool kAgain = kAsync && SLOTS > 1;         // longer rows are decoded a second time: their registers hold dgamma
-    const int threads = blockDim.x, per_stage = SLOTS * kPer * threads;
-    const int tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
+    const int threads = blockDim.x, tpr = p.tpr, at_once = threads / tpr, which = threadIdx.x / tpr, t = threadIdx.x - which * tpr;
     const int64_t step = (int64_t)gridDim.x * at_once;
     int64_t row = (int64_t)blockIdx.x * at_once + which;
     int half = 0;
-    const int ch0 = first_channel<SPREAD>(t);
+    const int ch0 = t * kGroup;
     float dg[SLOTS][16], gamma[16];
 #pragma unroll
     for (int s = 0; s < SLOTS; s++)
 #pragma unroll
         for (int i = 0; i < 16; i++) dg[s][i] = 0.f;
     pdl_enter();
-    load_gamma<SPREAD>(p, ch0, gamma);
+    load_gamma<ROWS>(p, ch0, gamma);
     // the lanes of this warp that share the row, their first channel, and where their chunks lie in a part of a stage (one per thread)
     const int lanes = tpr < 32 ? tpr : 32, lane = t & (lanes - 1), chw = (t - lane) * kGroup, mine = (int)threadIdx.x - lane;
+    // shifted rows have a chunk more per row and warp, in each part of a stage
+    const int extra = ROWS == kShifted ? mine / lanes : 0, extras = ROWS == kShifted ? threads / lanes : 0;
+    const int per_slot = kPer * threads + 3 * extras, per_stage = SLOTS * per_slot;
     auto fetch = [&](int stage, int64_t at) {
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            uint4 *to = stages + stage * per_stage + s * kPer * threads;
+            uint4 *to = stages + stage * per_stage + s * per_slot;
             const int ch = chw + s * tpr * kGroup, left = at < p.rows ? p.channels - ch : 0;
-            if (p.dh) fetch_row(to + mine * kS, lanes, lane, (const TS *)p.dh + (at * p.ld_s + ch), left);
-            fetch_row(to + kS * threads + mine * kB, lanes, lane, (const TB *)p.dn + (at * p.ld_b + ch), left);
-            if constexpr (FROM_H) fetch_row(to + (kS + kB) * threads + mine * kS, lanes, lane, (const TS *)p.x + (at * p.ld_s + ch), left);
-            else copy16(to + (kS + kB) * threads + threadIdx.x, p.ck.codes + (at * p.ck.pitch + ch + lane * kGroup), lane * kGroup < left);
+            if (p.dh) fetch_row<ROWS>(to + mine * kS + extra, lanes, lane, (const TS *)p.dh, at * p.ld_s + ch, left);
+            fetch_row<ROWS>(to + kS * threads + extras + mine * kB + extra, lanes, lane, (const TB *)p.dn, at * p.ld_b + ch, left);
+            if constexpr (FROM_H) fetch_row<ROWS>(to + (kS + kB) * threads + 2 * extras + mine * kS + extra, lanes, lane, (const TS *)p.x, at * p.ld_s + ch, left);
+            else copy16(to + (kS + kB) * threads + 2 * extras + threadIdx.x, p.ck.codes + (at * p.ck.pitch + ch + lane * kGroup), lane * kGroup < left ? 16 : 0);
         }
         copies_commit();
     };
@@ -225,16 +231,16 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
         }
     };
     // what the sums and dx need of slot s, out of a stage
-    auto staged_row = [&](int stage, int s, float (&x)[16], float (&dn)[16]) {
-        const uint4 *from = stages + stage * per_stage + s * kPer * threads;
+    auto staged_row = [&](int stage, int s, int64_t at_s, int64_t at_b, float (&x)[16], float (&dn)[16]) {
+        const uint4 *from = stages + stage * per_stage + s * per_slot;
         Raw16<TB> rn;
-        fetched(from + kS * threads + mine * kB, lane, rn);
+        fetched<ROWS>(from + kS * threads + extras + mine * kB + extra, lanes, lane, (const TB *)p.dn + at_b, rn);
         unpack(rn, dn);
         if constexpr (FROM_H) {
             Raw16<TS> rx;
-            fetched(from + (kS + kB) * threads + mine * kS, lane, rx);
+            fetched<ROWS>(from + (kS + kB) * threads + 2 * extras + mine * kS + extra, lanes, lane, (const TS *)p.x + at_s, rx);
             unpack(rx, x);
-        } else decode16<CODE>(from[(kS + kB) * threads + threadIdx.x], bytes[s], x);
+        } else decode16<CODE>(from[(kS + kB) * threads + 2 * extras + threadIdx.x], bytes[s], x);
     };
     ahead(row);
     for (int64_t row0 = (int64_t)blockIdx.x * at_once; row0 < p.rows; row0 += step, row += step) {
@@ -249,15 +255,15 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
         if constexpr (kAsync) { next_row_wait(p.stages); __syncwarp(); }
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
+            const int ch = (s * tpr + t) * kGroup, left = row_ok ? p.channels - ch : 0;
             const int k = kAgain ? 0 : s;
-            if constexpr (kAsync) staged_row(stage, s, x[k], dn[k]);
+            if constexpr (kAsync) staged_row(stage, s, at_s, at_b, x[k], dn[k]);
             else {
-                load16<SPREAD>((const TB *)p.dn + (at_b + ch), left, p.wide, dn[k]);
-                if constexpr (FROM_H) load16<SPREAD>((const TS *)p.x + (at_s + ch), left, p.wide, x[k]);
-                else read16<SPREAD, CODE>(p.ck, row, ch, left, x[k]);
+                load16<ROWS>((const TB *)p.dn + (at_b + ch), ch, left, p.wide, dn[k]);
+                if constexpr (FROM_H) load16<ROWS>((const TS *)p.x + (at_s + ch), ch, left, p.wide, x[k]);
+                else read16<CODE>(p.ck, row, ch, left, x[k]);
             }
-            if (s > 0) load_gamma<SPREAD>(p, ch, gamma);
+            if (s > 0) load_gamma<ROWS>(p, ch, gamma);
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 if constexpr (FROM_H) {
@@ -281,20 +287,20 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
         const float back = -sum[0] * p.inv_c * rstd * (FROM_H ? rstd * rstd : 1.f);
 #pragma unroll
         for (int s = 0; s < SLOTS; s++) {
-            const int ch = first_channel<SPREAD>(s * tpr + t), left = row_ok ? p.channels - ch : 0;
+            const int ch = (s * tpr + t) * kGroup, left = row_ok ? p.channels - ch : 0;
             float d[16];
             if (p.dh) {
                 Raw16<TS> rh;
-                if constexpr (kAsync) fetched(stages + stage * per_stage + s * kPer * threads + mine * kS, lane, rh);
-                else load_raw<SPREAD>((const TS *)p.dh + (at_s + ch), left, p.wide, rh);
+                if constexpr (kAsync) fetched<ROWS>(stages + stage * per_stage + s * per_slot + mine * kS + extra, lanes, lane, (const TS *)p.dh + at_s, rh);
+                else load_raw<ROWS>((const TS *)p.dh + (at_s + ch), ch, left, p.wide, rh);
                 unpack(rh, d);
             } else {
 #pragma unroll
                 for (int i = 0; i < 16; i++) d[i] = 0.f;
             }
             const int k = kAgain ? 0 : s;
-            if (SLOTS > 1 && (FROM_H || kAgain)) load_gamma<SPREAD>(p, ch, gamma);
-            if constexpr (kAgain) staged_row(stage, s, x[0], dn[0]);
+            if (SLOTS > 1 && (FROM_H || kAgain)) load_gamma<ROWS>(p, ch, gamma);
+            if constexpr (kAgain) staged_row(stage, s, at_s, at_b, x[0], dn[0]);
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 float w = dn[k][i] * rstd;
@@ -302,10 +308,10 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
                 if constexpr (FROM_H || kAgain) w *= gamma[i];
                 d[i] = fmaf(x[k][i], back, d[i] + w);
             }
-            store16<SPREAD>((TS *)p.dx + (at_s + ch), left, p.wide, d);
-            if (p.dr) store16<SPREAD>((TB *)p.dr + (at_b + ch), left, p.wide, d);
+            store16<ROWS>((TS *)p.dx + (at_s + ch), ch, left, p.wide, d);
+            if (p.dr) store16<ROWS>((TB *)p.dr + (at_b + ch), ch, left, p.wide, d);
         }
-        if (SLOTS > 1) load_gamma<SPREAD>(p, ch0, gamma);
+        if (SLOTS > 1) load_gamma<ROWS>(p, ch0, gamma);
         if constexpr (kAsync) { if (++stage == p.stages) stage = 0; }
     }
     if constexpr (kAsync) copies_wait<0>();
@@ -316,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
         float *sums = reinterpret_cast<float *>(stages);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; i++) sums[(threadIdx.x - t) * 16 + ch0 + step_of<SPREAD>(i)] = dg[0][i];
+        for (int i = 0; i < 16; i++) sums[(threadIdx.x - t) * 16 + ch0 + i] = dg[0][i];
         __syncthreads();
         for (int c = threadIdx.x; c < p.channels; c += threads) {
             float v = 0.f;
@@ -327,9 +333,9 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_bwd_kerne
     }
 #pragma unroll
     for (int s = 0; s < SLOTS; s++) {
-        const int ch = first_channel<SPREAD>(s * tpr + t);
+        const int ch = (s * tpr + t) * kGroup;
 #pragma unroll
-        for (int i = 0; i < 16; i++) if (ch + step_of<SPREAD>(i) < p.channels) out[ch + step_of<SPREAD>(i)] = dg[s][i];
+        for (int i = 0; i < 16; i++) if (ch + i < p.channels) out[ch + i] = dg[s][i];
     }
 }
 
@@ -350,9 +356,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_dgamma_kernel(const float *parti
 
 // 16-channel groups of a row -> threads per row (a power of two, or whole warps), groups per thread, threads per CTA, and the most of them
 struct Shape { int tpr, slots, threads, most; };
-Shape shape_of(int channels, bool spread) {
+Shape shape_of(int channels) {
     const int groups = ck_pitch(channels) / kGroup;
-    Shape s{spread ? 32 : 2, groups > 512 ? 2 : 1, 0, groups > 256 ? 512 : 256};       // at least the two lanes of a block of 32, or a warp
+    Shape s{2, groups > 512 ? 2 : 1, 0, groups > 256 ? 512 : 256};       // at least the two lanes of a block of 32
     const int need = (groups + s.slots - 1) / s.slots;
     while (s.tpr < need && s.tpr < 32) s.tpr *= 2;
     if (s.tpr < need) s.tpr = (need + 31) / 32 * 32;
@@ -367,60 +373,61 @@ int grid_of(const revnet_ctx *ctx, int64_t rows, const Shape &s, int per_sm) {
 // CTAs per SM and the stages of each, for rows that take `row` chunks per thread: as many CTAs as threads fit (`full` of the most threads), then
 // up to kMaxStages stages, as long as the rows in them stay within `bytes` per SM.
 struct Plan { int per_sm, stages; };
-Plan plan_of(const Shape &s, int channels, int row, int full, int bytes) {
-    const int used = s.threads / s.tpr * ((channels + kGroup - 1) / kGroup) * row * 16, stage = s.threads * s.slots * row * 16;
+int stage_bytes(int rows, const Shape &s, int row) { return s.slots * (s.threads * row + (rows == kShifted ? 3 * s.threads / std::min(s.tpr, 32) : 0)) * 16; }
+Plan plan_of(int rows, const Shape &s, int channels, int row, int full, int bytes) {
+    const int used = s.threads / s.tpr * ((channels + kGroup - 1) / kGroup) * row * 16, stage = stage_bytes(rows, s, row);
     Plan p{full * s.most / s.threads, 2};
     while (p.per_sm > 1 && (p.per_sm * 2 * used > bytes || 2 * stage > shared_of(p.per_sm))) p.per_sm--;
     while (p.stages < kMaxStages && p.per_sm * (p.stages + 1) * used <= bytes && (p.stages + 1) * stage <= shared_of(p.per_sm)) p.stages++;
     return p;
 }
-Plan fwd_plan(const Shape &s, int channels, int row) { return plan_of(s, channels, row, per_sm_of(s.most), s.most == 512 ? kFwdBytes : kFwdBytes - 1); }
-Plan bwd_plan(const Shape &s, int channels, int row) { return plan_of(s, channels, row, per_sm_of(s.most), kBwdBytes); }
+// (shifted rows take more instructions than bytes: as many as fit)
+Plan fwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : (s.most == 512 ? kFwdBytes : kFwdBytes - 1)); }
+Plan bwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : kBwdBytes); }
 template <class K> bool with_shared(Exec &ex, OncePerDevice &once, K kernel, size_t bytes) {
     if (!once.first(ex.ctx->device)) return true;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
-// records of dgamma: by the larger grid of the two forms, whose choice also depends on addresses
+// records of dgamma, of the largest grid that a call may have: its rows' alignment decides too
 int parts_of(const revnet_ctx *ctx, const revnet_norm_desc &d) {
-    const Shape a = shape_of(d.channels, false), b = shape_of(d.channels, true);
-    const int ga = grid_of(ctx, d.rows, a, bwd_plan(a, d.channels, 1).per_sm), gb = grid_of(ctx, d.rows, b, bwd_plan(b, d.channels, 1).per_sm);
-    return ga > gb ? ga : gb;
+    const Shape s = shape_of(d.channels);
+    return grid_of(ctx, d.rows, s, per_sm_of(s.most) * s.most / s.threads);
 }
 
-template <bool SPREAD, class TS, class TB, int CODE, int SLOTS, int THREADS> void fwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
+template <int ROWS, class TS, class TB, int CODE, int SLOTS, int THREADS> void fwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
     static OncePerDevice once;
     constexpr int row = kChunks<TS> + kChunks<TB>;
-    constexpr bool async = staged(SPREAD, SLOTS * row * THREADS);
-    p.stages = fwd_plan(s, p.channels, row).stages;
-    if (!with_shared(ex, once, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, async ? shared_of(1) : 0)) return;
-    launch_stream(ex, bytes, async ? 100 : 0, rmsnorm_fwd_kernel<SPREAD, TS, TB, CODE, SLOTS, THREADS>, grid, s.threads, async ? (size_t)p.stages * s.threads * SLOTS * row * 16 : 0, p);
+    constexpr bool async = staged(ROWS, SLOTS, row, THREADS);
+    p.stages = fwd_plan(ROWS, s, p.channels, row).stages;
+    if (!with_shared(ex, once, rmsnorm_fwd_kernel<ROWS, TS, TB, CODE, SLOTS, THREADS>, async ? shared_of(1) : 0)) return;
+    launch_stream(ex, bytes, async ? 100 : 0, rmsnorm_fwd_kernel<ROWS, TS, TB, CODE, SLOTS, THREADS>, grid, s.threads, async ? (size_t)p.stages * stage_bytes(ROWS, s, row) : 0, p);
 }
-template <bool SPREAD, class TS, class TB, int CODE> void fwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
-    if (s.slots == 2) fwd_k<SPREAD, TS, TB, CODE, 2, 512>(ex, p, s, grid, bytes);
-    else if (s.most == 512) fwd_k<SPREAD, TS, TB, CODE, 1, 512>(ex, p, s, grid, bytes);
-    else fwd_k<SPREAD, TS, TB, CODE, 1, 256>(ex, p, s, grid, bytes);
+template <int ROWS, class TS, class TB, int CODE> void fwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
+    if (s.slots == 2) fwd_k<ROWS, TS, TB, CODE, 2, 512>(ex, p, s, grid, bytes);
+    else if (s.most == 512) fwd_k<ROWS, TS, TB, CODE, 1, 512>(ex, p, s, grid, bytes);
+    else fwd_k<ROWS, TS, TB, CODE, 1, 256>(ex, p, s, grid, bytes);
 }
-template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS> void bwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
+template <int ROWS, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int THREADS> void bwd_k(Exec &ex, NormArgs p, const Shape &s, unsigned grid, double bytes) {
     static OncePerDevice once;
     constexpr int row = kChunks<TS> + kChunks<TB> + (FROM_H ? kChunks<TS> : 1);
-    constexpr bool async = staged(SPREAD, SLOTS * row * THREADS);
-    p.stages = bwd_plan(s, p.channels, row).stages;
-    const size_t rows = async ? (size_t)p.stages * s.threads * SLOTS * row * 16 : 0, least = THREADS == 256 ? THREADS * 16 * sizeof(float) : 0, smem = rows > least ? rows : least;
-    if (!with_shared(ex, once, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, async ? shared_of(1) : least)) return;
-    launch_stream(ex, bytes, async ? 100 : 15, rmsnorm_bwd_kernel<SPREAD, TS, TB, FROM_H, CODE, SLOTS, THREADS>, grid, s.threads, smem, p);
+    constexpr bool async = staged(ROWS, SLOTS, row, THREADS);
+    p.stages = bwd_plan(ROWS, s, p.channels, row).stages;
+    const size_t rows = async ? (size_t)p.stages * stage_bytes(ROWS, s, row) : 0, least = THREADS == 256 ? THREADS * 16 * sizeof(float) : 0, smem = rows > least ? rows : least;
+    if (!with_shared(ex, once, rmsnorm_bwd_kernel<ROWS, TS, TB, FROM_H, CODE, SLOTS, THREADS>, async ? shared_of(1) : least)) return;
+    launch_stream(ex, bytes, async ? 100 : 15, rmsnorm_bwd_kernel<ROWS, TS, TB, FROM_H, CODE, SLOTS, THREADS>, grid, s.threads, smem, p);
 }
-template <bool SPREAD, class TS, class TB, bool FROM_H, int CODE> void bwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
-    if (s.slots == 2) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 2, 512>(ex, p, s, grid, bytes);
-    else if (s.most == 512) bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 512>(ex, p, s, grid, bytes);
-    else bwd_k<SPREAD, TS, TB, FROM_H, CODE, 1, 256>(ex, p, s, grid, bytes);
+template <int ROWS, class TS, class TB, bool FROM_H, int CODE> void bwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
+    if (s.slots == 2) bwd_k<ROWS, TS, TB, FROM_H, CODE, 2, 512>(ex, p, s, grid, bytes);
+    else if (s.most == 512) bwd_k<ROWS, TS, TB, FROM_H, CODE, 1, 512>(ex, p, s, grid, bytes);
+    else bwd_k<ROWS, TS, TB, FROM_H, CODE, 1, 256>(ex, p, s, grid, bytes);
 }
-template <class F> void by_types(const revnet_norm_desc &d, bool spread, F &&f) {
+template <class F> void by_types(const revnet_norm_desc &d, int rows, F &&f) {
     auto types = [&](auto s) {
         if (d.stream_dtype == REVNET_BF16) f(s, bf16(), bf16());
         else if (d.branch_dtype == REVNET_BF16) f(s, float(), bf16());
         else f(s, float(), float());
     };
-    if (spread) types(std::true_type()); else types(std::false_type());
+    if (rows == kPieces) types(std::integral_constant<int, kPieces>()); else types(std::integral_constant<int, kShifted>());
 }
 NormArgs args_of(const revnet_norm_desc &d) {
     NormArgs p{};
@@ -439,13 +446,13 @@ void rmsnorm_fwd(Exec &ex, const revnet_norm_desc &d, const void *x, const void 
     p.x = x; p.r = r; p.gamma = gamma; p.h = h; p.n = n; p.rstd = rstd; p.ck = ck_view(ck, d.rows, d.channels);
     const int access = std::min({row_access(x, d.ld_stream, ss, d.channels), row_access(h, d.ld_stream, ss, d.channels), row_access(r, d.ld_branch, sb, d.channels),
                                  row_access(n, d.ld_branch, sb, d.channels), row_access(gamma, 0, 4, d.channels)});
-    const bool spread = access == 0;
+    const int rows = access ? kPieces : kShifted;
     p.wide = access == 2;
-    const Shape s = shape_of(d.channels, spread);
+    const Shape s = shape_of(d.channels);
     p.tpr = s.tpr;
     const double bytes = (double)d.rows * d.channels * (ss + (r ? sb : 0) + (h ? ss : 0) + (n ? sb : 0) + (ck ? 1 : 0));
-    const unsigned grid = (unsigned)grid_of(ex.ctx, d.rows, s, fwd_plan(s, d.channels, ss + sb).per_sm);
-    by_types(d, spread, [&](auto sp, auto ts, auto tb) {
+    const unsigned grid = (unsigned)grid_of(ex.ctx, d.rows, s, fwd_plan(rows, s, d.channels, ss + sb).per_sm);
+    by_types(d, rows, [&](auto sp, auto ts, auto tb) {
         if (d.code == REVNET_INT8) fwd_t<decltype(sp)::value, decltype(ts), decltype(tb), REVNET_INT8>(ex, p, s, grid, bytes);
         else fwd_t<decltype(sp)::value, decltype(ts), decltype(tb), REVNET_E4M3>(ex, p, s, grid, bytes);
     });
@@ -462,14 +469,14 @@ void rmsnorm_bwd(Exec &ex, const revnet_norm_desc &d, const void *dn, const void
     p.ck = ck_view(ck, d.rows, d.channels);
     const int access = std::min({row_access(h, d.ld_stream, ss, d.channels), row_access(dh, d.ld_stream, ss, d.channels), row_access(dx, d.ld_stream, ss, d.channels),
                                  row_access(dn, d.ld_branch, sb, d.channels), row_access(dr, d.ld_branch, sb, d.channels), row_access(gamma, 0, 4, d.channels)});
-    const bool spread = access == 0;
+    const int rows = access ? kPieces : kShifted;
     p.wide = access == 2;
-    const Shape s = shape_of(d.channels, spread);
+    const Shape s = shape_of(d.channels);
     p.tpr = s.tpr;
-    const int grid = grid_of(ex.ctx, d.rows, s, bwd_plan(s, d.channels, h ? ss + sb + ss : ss + sb + 1).per_sm);
+    const int grid = grid_of(ex.ctx, d.rows, s, bwd_plan(rows, s, d.channels, h ? ss + sb + ss : ss + sb + 1).per_sm);
     if (grid > 0) {
         const double bytes = (double)d.rows * d.channels * (sb + (dh ? ss : 0) + (h ? ss : 1) + ss + (dr ? sb : 0));
-        by_types(d, spread, [&](auto sp, auto ts, auto tb) {
+        by_types(d, rows, [&](auto sp, auto ts, auto tb) {
             if (h) bwd_t<decltype(sp)::value, decltype(ts), decltype(tb), true, 0>(ex, p, s, grid, bytes);
             else if (d.code == REVNET_INT8) bwd_t<decltype(sp)::value, decltype(ts), decltype(tb), false, REVNET_INT8>(ex, p, s, grid, bytes);
             else bwd_t<decltype(sp)::value, decltype(ts), decltype(tb), false, REVNET_E4M3>(ex, p, s, grid, bytes);

@@ -61,22 +61,69 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t byte_of(const uint8_t *p) { return *p; }
 
-// A thread's 16 channels.  Rows of 16-byte pieces on 16-byte boundaries: 16 consecutive ones, moved by accesses of 32 (`wide`) or 16 bytes.  Any
-// other rows (SPREAD): every 32nd of 512, the lanes of a warp side by side, so that a warp's accesses are whole lines where a thread's
-// would be an element each.  `left` is the row's length minus the thread's first channel.
+// A thread's 16 channels.
+//   kPieces   rows of 16-byte pieces on 16-byte boundaries: 16 consecutive ones, moved by accesses of 32 (`wide`) or 16 bytes
+//   kShifted  any other rows: 16 consecutive ones too, loaded as the aligned 16 bytes that hold them and shifted into place; stored the same way, with
+//             the end of the lane before.  Elements one by one only at the ends of a row (stores: of a warp's part of it)
+//   kCut      the same, of gated rows whose second half's codes start inside 16
+// `left` is the row's length minus the thread's first channel.
 constexpr int kGroup = 16;
-template <bool SPREAD> __device__ __forceinline__ int first_channel(int t) { return SPREAD ? (t & ~31) * kGroup + (t & 31) : t * kGroup; }
-template <bool SPREAD> __device__ __forceinline__ int step_of(int i) { return SPREAD ? 32 * i : i; }
+enum { kPieces, kShifted, kCut };
 
 // raw words of 16 elements, so that a load can be in flight while earlier values are worked on
 template <class T> struct Raw16 { uint32_t w[16 * sizeof(T) / 4]; };
 __device__ __forceinline__ uint32_t bits_of(const float *p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits_of(const bf16 *p) { return *reinterpret_cast<const uint16_t *>(p); }
 
+// r = w from `bytes` (0 to 16, a multiple of SIZE) on; w holds four words more than r.  (A branch for each whole word instead of the selections
+// saves nothing: 8192 x 2500 norms in bf16 54.6 and 55.4 us forward, float32 with rows of 100 channels 10 % slower.)
+template <int SIZE, int N, int W> __device__ __forceinline__ void shift_words(uint32_t (&w)[N], uint32_t bytes, uint32_t (&r)[W]) {
+    static_assert(N == W + 4, "");
+    if (bytes & 16u) {
+#pragma unroll
+        for (int i = 0; i < N - 4; i++) w[i] = w[i + 4];
+    }
+    if (bytes & 8u) {
+#pragma unroll
+        for (int i = 0; i < N - 2; i++) w[i] = w[i + 2];
+    }
+    if (bytes & 4u) {
+#pragma unroll
+        for (int i = 0; i < N - 1; i++) w[i] = w[i + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < W; i++) r[i] = SIZE < 4 ? __funnelshift_r(w[i], w[i + 1], 8u * (bytes & (SIZE == 2 ? 2u : 3u))) : w[i];
+}
+// kShifted, reads nothing outside the row; ch: p's channel (0: the row's start)
+template <class T> __device__ __forceinline__ void load_shifted(const T *p, int ch, int left, Raw16<T> &r) {
+    constexpr int kSize = sizeof(T), kN = kSize + 1, kBytes = 16 * kSize;       // aligned pieces
+    const uint32_t o = (uint32_t)(uintptr_t)p & 15u;
+    const char *from = reinterpret_cast<const char *>(p) - o;
+    const int first = ch == 0 ? 0 : -16, end = left * kSize;
+    uint32_t w[4 * kN];
+#pragma unroll
+    for (int k = 0; k < kN; k++) {
+        const int at = 16 * k - (int)o;
+        uint4 q = make_uint4(0u, 0u, 0u, 0u);
+        if (at >= first && at + 16 <= end) { if (at < kBytes) q = *reinterpret_cast<const uint4 *>(from + 16 * k); }
+        else if (at < end && at < kBytes) {
+            uint32_t e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < 16 / kSize; j++)
+                if (at + j * kSize >= 0 && at + j * kSize < end)
+                    e[j * kSize / 4] |= bits_of(reinterpret_cast<const T *>(from + 16 * k) + j) << (8 * (j * kSize & 3));
+            q = make_uint4(e[0], e[1], e[2], e[3]);
+        }
+        w[4 * k] = q.x; w[4 * k + 1] = q.y; w[4 * k + 2] = q.z; w[4 * k + 3] = q.w;
+    }
+    shift_words<kSize>(w, o, r.w);
+}
+
 // elements of p (the thread's first channel), zeros where there is none
-template <bool SPREAD, class T> __device__ __forceinline__ void load_raw(const T *p, int left, bool wide, Raw16<T> &r) {
+template <int ROWS, class T> __device__ __forceinline__ void load_raw(const T *p, int ch, int left, bool wide, Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
-    if constexpr (!SPREAD) {
+    if constexpr (ROWS != kPieces) load_shifted(p, ch, left, r);
+    else {
         if (left >= 16 && wide) {
 #pragma unroll
             for (int i = 0; i < W; i += 8) {
@@ -92,12 +139,6 @@ template <bool SPREAD, class T> __device__ __forceinline__ void load_raw(const T
                 if (i * 4 / (int)sizeof(T) < left) q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) + 4 * i);
                 r.w[i] = q.x; r.w[i + 1] = q.y; r.w[i + 2] = q.z; r.w[i + 3] = q.w;
             }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; i++) {
-            if constexpr (sizeof(T) == 4) r.w[i] = 32 * i < left ? bits_of(p + 32 * i) : 0u;
-            else r.w[i] = (64 * i < left ? bits_of(p + 64 * i) : 0u) | (64 * i + 32 < left ? bits_of(p + 64 * i + 32) : 0u) << 16;
         }
     }
 }
@@ -120,9 +161,47 @@ __device__ __forceinline__ void pack(const float (&v)[16], Raw16<bf16> &r) {
 }
 __device__ __forceinline__ void put_bits(float *p, uint32_t w) { *p = __uint_as_float(w); }
 __device__ __forceinline__ void put_bits(bf16 *p, uint32_t w) { *reinterpret_cast<uint16_t *>(p) = (uint16_t)w; }
-template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, int left, bool wide, const Raw16<T> &r) {
+// kShifted: all lanes of the warp call it, neighbours that share a row with neighbouring groups of it
+template <class T> __device__ __forceinline__ void store_shifted(T *p, int ch, int left, const Raw16<T> &r) {
+    constexpr int kSize = sizeof(T), W = 4 * kSize, kBytes = 16 * kSize;
+    const int o = (int)((uint32_t)(uintptr_t)p & 15u), lane = threadIdx.x & 31, n = left >= 16 ? kBytes : (left > 0 ? left * kSize : 0);
+    char *to = reinterpret_cast<char *>(p) - o;
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = __shfl_up_sync(0xffffffffu, r.w[W - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < W; i++) w[4 + i] = r.w[i];
+    uint32_t v[W];
+    shift_words<kSize>(w, 16u - o, v);
+    // the first piece holds the end of the lane before, if that has one; the last elements go with the next lane's first piece, if that is whole
+    const bool head = o == 0 || (lane > 0 && ch > 0), tail = o == 0 || (lane < 31 && left * kSize - kBytes >= 16 - o);
+#pragma unroll
+    for (int k = 0; k < kSize; k++)
+        if ((k > 0 || head) && 16 * k + 16 - o <= n) *reinterpret_cast<uint4 *>(to + 16 * k) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    auto put = [&](int i) { put_bits(p + i, r.w[i * kSize / 4] >> (8 * (i * kSize & 3))); };
+    if (n < kBytes) {                // the row's end
+        if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int piece = (i * kSize + o) >> 4;
+                if (i * kSize < n && (16 * piece + 16 - o > n || (piece == 0 && !head))) put(i);
+            }
+        }
+        return;
+    }
+    if (!head) {
+#pragma unroll
+        for (int i = 0; i < 16 / kSize; i++) if (i * kSize < 16 - o) put(i);
+    }
+    if (!tail) {
+#pragma unroll
+        for (int i = 16 - 16 / kSize; i < 16; i++) if (i * kSize >= kBytes - o) put(i);
+    }
+}
+template <int ROWS, class T> __device__ __forceinline__ void store_raw(T *p, int ch, int left, bool wide, const Raw16<T> &r) {
     constexpr int W = 16 * sizeof(T) / 4;
-    if constexpr (!SPREAD) {
+    if constexpr (ROWS != kPieces) store_shifted(p, ch, left, r);
+    else {
         if (left >= 16 && wide) {
 #pragma unroll
             for (int i = 0; i < W; i += 8) {
@@ -137,21 +216,17 @@ template <bool SPREAD, class T> __device__ __forceinline__ void store_raw(T *p, 
                 if (i * 4 / (int)sizeof(T) < left)
                     *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p) + 4 * i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; i++)
-            if (32 * i < left) put_bits(p + 32 * i, sizeof(T) == 4 ? r.w[i * sizeof(T) / 4] : r.w[i / 2] >> (16 * (i & 1)));
     }
 }
-template <bool SPREAD, class T> __device__ __forceinline__ void load16(const T *p, int left, bool wide, float (&v)[16]) {
+template <int ROWS, class T> __device__ __forceinline__ void load16(const T *p, int ch, int left, bool wide, float (&v)[16]) {
     Raw16<T> r;
-    load_raw<SPREAD>(p, left, wide, r);
+    load_raw<ROWS>(p, ch, left, wide, r);
     unpack(r, v);
 }
-template <bool SPREAD, class T> __device__ __forceinline__ void store16(T *p, int left, bool wide, const float (&v)[16]) {
+template <int ROWS, class T> __device__ __forceinline__ void store16(T *p, int ch, int left, bool wide, const float (&v)[16]) {
     Raw16<T> r;
     pack(v, r);
-    store_raw<SPREAD>(p, left, wide, r);
+    store_raw<ROWS>(p, ch, left, wide, r);
 }
 
 // ---------------------------------------------------------------- rows on their way
@@ -159,27 +234,59 @@ template <bool SPREAD, class T> __device__ __forceinline__ void store16(T *p, in
 // while they are in flight.  The lanes of a warp that share a row (`lanes` of them, 16 channels each) copy side by side, whole lines per
 // instruction, and wait for each other (__syncwarp behind the wait) before a thread reads its own 16 channels.  A thread's chunks are
 // neighbours, so eight lanes that read their k-th chunk would meet in half or a quarter of the banks: chunk c lies at c ^ (bits 3.. of c).
-// Not for SPREAD.
-__device__ __forceinline__ void copy16(void *dst, const void *src, bool in) {        // in = false: zeros, nothing is read
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
+// kShifted: the aligned chunks that hold the channels, one more than their number (which lies behind them as it is); the first may start with
+// the end of the row before, or with what lies between the rows, but with nothing in front of the tensor.
+__device__ __forceinline__ void copy16(void *dst, const void *src, int bytes) {       // bytes of src, zeros behind them (0: nothing is read)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 template <class T> constexpr int kChunks = 16 * (int)sizeof(T) / 16;
 template <class T> __device__ __forceinline__ int chunk_place(int c) { return c ^ ((c >> 3) & (kChunks<T> - 1)); }
-// p: the first of the lanes' channels, `left` of them in the row; to: the lanes' part of a stage
-template <class T> __device__ __forceinline__ void fetch_row(uint4 *to, int lanes, int lane, const T *p, int left) {
+// at: the first of the lanes' channels in the tensor, `left` of them in the row; to: the lanes' part of a stage
+template <int ROWS, class T> __device__ __forceinline__ void fetch_row(uint4 *to, int lanes, int lane, const T *tensor, int64_t at, int left) {
+    const char *p = reinterpret_cast<const char *>(tensor + at);
+    if constexpr (ROWS == kPieces) {
 #pragma unroll
-    for (int k = 0; k < kChunks<T>; k++) {
-        const int c = k * lanes + lane;
-        copy16(to + chunk_place<T>(c), reinterpret_cast<const char *>(p) + 16 * c, c * (16 / (int)sizeof(T)) < left);
+        for (int k = 0; k < kChunks<T>; k++) {
+            const int c = k * lanes + lane;
+            copy16(to + chunk_place<T>(c), p + 16 * c, c * (16 / (int)sizeof(T)) < left ? 16 : 0);
+        }
+    } else {
+        const int o = (int)((uint32_t)(uintptr_t)p & 15u), bytes = left > 0 ? left * (int)sizeof(T) + o : 0;
+        p -= o;
+        auto in = [&](int c) { const int n = bytes - 16 * c; return n < 0 ? 0 : (n < 16 ? n : 16); };
+        const bool front = lane == 0 && bytes > 0 && p < reinterpret_cast<const char *>(tensor);
+#pragma unroll
+        for (int k = 0; k < kChunks<T>; k++) {
+            const int c = k * lanes + lane;
+            if (k > 0 || !front) copy16(to + chunk_place<T>(c), p + 16 * c, in(c));
+        }
+        if (lane == 0) copy16(to + kChunks<T> * lanes, p + 16 * kChunks<T> * lanes, o ? in(kChunks<T> * lanes) : 0);
+        if (front) {
+            uint32_t e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < 16 / (int)sizeof(T); j++)
+                if (j * (int)sizeof(T) >= o && j * (int)sizeof(T) < bytes)
+                    e[j * sizeof(T) / 4] |= bits_of(reinterpret_cast<const T *>(p) + j) << (8 * (j * sizeof(T) & 3));
+            to[0] = make_uint4(e[0], e[1], e[2], e[3]);
+        }
     }
 }
-template <class T> __device__ __forceinline__ void fetched(const uint4 *from, int lane, Raw16<T> &r) {
+// row: any address that is a multiple of 16 channels away from the row's start
+template <int ROWS, class T> __device__ __forceinline__ void fetched(const uint4 *from, int lanes, int lane, const T *row, Raw16<T> &r) {
+    constexpr int W = 4 * kChunks<T>;
+    uint32_t w[W + 4];
 #pragma unroll
-    for (int k = 0; k < kChunks<T>; k++) {
-        const uint4 q = from[chunk_place<T>(lane * kChunks<T> + k)];
-        r.w[4 * k] = q.x; r.w[4 * k + 1] = q.y; r.w[4 * k + 2] = q.z; r.w[4 * k + 3] = q.w;
+    for (int k = 0; k < kChunks<T> + (ROWS == kShifted); k++) {
+        const int c = lane * kChunks<T> + k;
+        const uint4 q = from[k == kChunks<T> && lane == lanes - 1 ? c : chunk_place<T>(c)];
+        w[4 * k] = q.x; w[4 * k + 1] = q.y; w[4 * k + 2] = q.z; w[4 * k + 3] = q.w;
+    }
+    if constexpr (ROWS == kShifted) shift_words<sizeof(T)>(w, (uint32_t)(uintptr_t)row & 15u, r.w);
+    else {
+#pragma unroll
+        for (int i = 0; i < W; i++) r.w[i] = w[i];
     }
 }
 
@@ -250,55 +357,22 @@ template <int CODE> __device__ __forceinline__ void decode16(uint4 q, uint32_t b
 __device__ __forceinline__ size_t scale_index(const Checkpoint &ck, size_t row, int ch) {
     return ((size_t)(ch >> 7) * ck.rows_pad + row) * 4 + ((ch >> 5) & 3);
 }
-// 16 channels into a checkpoint (all lanes of the warp call it, SPREAD: all of one row).  live: the row exists.  v holds zeros behind the row's
-// last channel.  end: first channel that is not to be written (a multiple of 32; 0: the padded row's end).
-template <bool SPREAD, int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16], int end = 0) {
+// 16 channels into a checkpoint (all lanes of the warp call it).  live: the row exists.  v holds zeros behind the row's last channel.  end: first
+// channel that is not to be written (a multiple of 32; 0: the padded row's end).
+template <int CODE> __device__ __forceinline__ void keep16(const Checkpoint &ck, size_t row, int ch, bool live, const float (&v)[16], int end = 0) {
     if (end == 0) end = ck.pitch;
-    if constexpr (SPREAD) {
-        // the lanes of a warp hold the 32 channels of a block; lane i writes the scale of block i
-        const int ch0 = ch & ~31, lane = ch & 31;
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            if (ch0 + 32 * i >= end) break;
-            const uint32_t byte = scale_byte<CODE>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
-            if (lane == i) mine = byte;
-            const float inv = __uint_as_float((254u - byte) << 23);
-            uint32_t c;
-            if constexpr (CODE == REVNET_INT8) c = __float_as_uint(__fmaf_rn(v[i], inv, 12582912.f));
-            else c = __nv_cvt_float_to_fp8(v[i] * inv, __NV_SATFINITE, __NV_E4M3);
-            if (live) ck.codes[row * ck.pitch + ch + 32 * i] = byte == 255u ? (uint8_t)0 : (uint8_t)c;
-        }
-        if (live && lane < 16 && ch0 + 32 * lane < end) ck.scales[scale_index(ck, row, ch0 + 32 * lane)] = (uint8_t)mine;
-    } else {
-        uint32_t top = abs_max16(v);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        const uint32_t byte = scale_byte<CODE>(top);
-        if (!live || ch >= end) return;
-        *reinterpret_cast<uint4 *>(ck.codes + row * ck.pitch + ch) = encode16<CODE>(v, byte);
-        if ((ch & 16) == 0) ck.scales[scale_index(ck, row, ch)] = (uint8_t)byte;
-    }
+    uint32_t top = abs_max16(v);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t byte = scale_byte<CODE>(top);
+    if (!live || ch >= end) return;
+    *reinterpret_cast<uint4 *>(ck.codes + row * ck.pitch + ch) = encode16<CODE>(v, byte);
+    if ((ch & 16) == 0) ck.scales[scale_index(ck, row, ch)] = (uint8_t)byte;
 }
-// 16 channels' codes, not yet decoded: 16 bytes and a scale byte, or (SPREAD) 16 bytes of 16 blocks and their scales
-template <bool SPREAD> struct RawCodes;
-template <> struct RawCodes<false> { uint4 q; uint32_t byte; };
-template <> struct RawCodes<true> { uint4 q, bytes; };
-// left as for load_raw; ch a multiple of 16 unless SPREAD
-template <bool SPREAD> __device__ __forceinline__ void load_codes(const Checkpoint &ck, size_t row, int ch, int left, RawCodes<SPREAD> &r) {
-    if constexpr (SPREAD) {
-        uint32_t c[4] = {0u, 0u, 0u, 0u}, b[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 16; i++)
-            if (32 * i < left) {
-                c[i / 4] |= byte_of(ck.codes + row * ck.pitch + ch + 32 * i) << (8 * (i & 3));
-                // the scales of four blocks are one word where the first is a multiple of four (always but in a gated row's second half); bytes behind the
-                // last block are not used
-                if (i % 4 == 0 && (ch & 96) == 0) b[i / 4] = *reinterpret_cast<const uint32_t *>(ck.scales + scale_index(ck, row, ch + 32 * i));
-                if ((ch & 96) != 0) b[i / 4] |= byte_of(ck.scales + scale_index(ck, row, ch + 32 * i)) << (8 * (i & 3));
-            }
-        r.q = make_uint4(c[0], c[1], c[2], c[3]);
-        r.bytes = make_uint4(b[0], b[1], b[2], b[3]);
-    } else if (left > 0) {
+// 16 channels' codes, not yet decoded
+struct RawCodes { uint4 q; uint32_t byte; };
+// left as for load_raw; ch a multiple of 16
+__device__ __forceinline__ void load_codes(const Checkpoint &ck, size_t row, int ch, int left, RawCodes &r) {
+    if (left > 0) {
         r.q = *reinterpret_cast<const uint4 *>(ck.codes + row * ck.pitch + ch);
         r.byte = byte_of(ck.scales + scale_index(ck, row, ch));
     } else {
@@ -306,17 +380,32 @@ template <bool SPREAD> __device__ __forceinline__ void load_codes(const Checkpoi
         r.byte = 0u;
     }
 }
-template <bool SPREAD, int CODE> __device__ __forceinline__ void decode(const RawCodes<SPREAD> &r, float (&v)[16]) {
-    if constexpr (SPREAD) {
-        decode16<CODE>(r.q, 127u, v);
-        const uint32_t b[4] = {r.bytes.x, r.bytes.y, r.bytes.z, r.bytes.w};
-#pragma unroll
-        for (int i = 0; i < 16; i++) v[i] *= __uint_as_float(((b[i / 4] >> (8 * (i & 3))) & 0xffu) << 23);
-    } else decode16<CODE>(r.q, r.byte, v);
+template <int CODE> __device__ __forceinline__ void decode(const RawCodes &r, float (&v)[16]) { decode16<CODE>(r.q, r.byte, v); }
+template <int CODE> __device__ __forceinline__ void read16(const Checkpoint &ck, size_t row, int ch, int left, float (&v)[16]) {
+    RawCodes r;
+    load_codes(ck, row, ch, left, r);
+    decode<CODE>(r, v);
 }
-template <bool SPREAD, int CODE> __device__ __forceinline__ void read16(const Checkpoint &ck, size_t row, int ch, int left, float (&v)[16]) {
-    RawCodes<SPREAD> r;
-    load_codes<SPREAD>(ck, row, ch, left, r);
-    decode<SPREAD, CODE>(r, v);
+// the same from any channel on: out of the two aligned pieces that hold them, under the scales of up to two blocks
+struct RawCodesAt { uint4 q; uint32_t byte, next; int cut; };            // next: the scale byte from the cut-th on
+__device__ __forceinline__ void load_codes_at(const Checkpoint &ck, size_t row, int ch, int left, RawCodesAt &r) {
+    r.q = make_uint4(0u, 0u, 0u, 0u);
+    r.byte = r.next = 0u;
+    r.cut = 32 - (ch & 31);
+    if (left <= 0) return;
+    const int at = ch & ~15;
+    const uint4 *from = reinterpret_cast<const uint4 *>(ck.codes + row * ck.pitch + at);
+    const uint4 a = from[0], b = at + 16 < (int)ck.pitch ? from[1] : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, c[4];
+    shift_words<1>(w, ch & 15u, c);
+    r.q = make_uint4(c[0], c[1], c[2], c[3]);
+    r.byte = byte_of(ck.scales + scale_index(ck, row, ch));
+    r.next = r.cut < left && r.cut < 16 ? byte_of(ck.scales + scale_index(ck, row, ch + r.cut)) : 0u;
+}
+template <int CODE> __device__ __forceinline__ void decode(const RawCodesAt &r, float (&v)[16]) {
+    decode16<CODE>(r.q, 127u, v);
+    const float s = __uint_as_float(r.byte << 23), t = __uint_as_float(r.next << 23);
+#pragma unroll
+    for (int i = 0; i < 16; i++) v[i] *= i < r.cut ? s : t;
 }
 #endif

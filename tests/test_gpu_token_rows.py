@@ -183,6 +183,44 @@ def test_activation_forward_and_backward(ctx, rows, channels, pad, skip, kind, c
         assert torch.equal(rx.t, keep)
 
 
+@pytest.mark.parametrize("skip", range(8))
+@pytest.mark.parametrize("channels,pad", [(16, 1), (45, 0), (528, 2), (1043, 0), (1056, 5)])
+def test_every_alignment_of_a_row(ctx, channels, pad, skip):
+    """Rows that start at every element of 16 bytes, and go on at others: nothing beside them is written, and values land where they belong."""
+    test_activation_forward_and_backward(ctx, 11, channels, pad, skip, "silu", "int8", "bf16")
+    test_activation_forward_and_backward(ctx, 11, channels, pad, skip, "relu", "e4m3", "f32")
+    test_norm_forward(ctx, 11, channels, pad, skip, "f32", "bf16", "int8")
+    test_norm_backward(ctx, 11, channels, pad, skip, "bf16", "bf16", "h")
+    test_norm_backward(ctx, 11, channels, pad, skip, "f32", "f32", "e4m3")
+
+
+@pytest.mark.parametrize("code,dtype", [("int8", "f32"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("half", [1, 4, 15, 16, 17, 20, 31, 33, 40, 520, 523, 2060])
+def test_gated_halves_of_any_length(ctx, half, code, dtype):
+    """The second half starts inside a block, inside 16 codes, and on neither's boundary."""
+    test_activation_forward_and_backward(ctx, 13, 2 * half, 0, 0, "swiglu", code, dtype)
+    test_activation_forward_and_backward(ctx, 13, 2 * half, 3, 1, "swiglu", code, dtype)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_a_bad_block_across_the_gate_stays_in_its_block(ctx, code):
+    half = 41                         # blocks of 32: the second one holds the end of g and the start of u
+    x = torch.ones(2, 2 * half)
+    x[0, 50] = math.nan
+    ck, a, da, dx, ack = Ck(2, 2 * half), Rows(2, half, "f32"), torch.ones(2, half).cuda(), Rows(2, 2 * half, "f32"), Ck(2, half)
+    d = B.act_desc(2, 2 * half, "f32", code, "swiglu")
+    B.revnet_act_store(ctx, d, x.cuda(), ck.t)
+    B.revnet_act_load(ctx, d, ck.t, a.t)
+    B.revnet_act_bwd(ctx, d, ck.t, da, dx.t, ack.t)
+    bad = torch.zeros(2 * half, dtype=torch.bool)
+    bad[32:64] = True                 # of g: 32 to 40; of u: 0 to 22
+    gone = bad[:half] | bad[half:]
+    assert torch.equal(torch.isnan(a.cpu())[0], gone) and not torch.isnan(a.cpu()[1]).any()
+    g = torch.isnan(dx.cpu())
+    assert torch.equal(g[0, :half], gone) and torch.equal(g[0, half:], bad[:half]) and not g[1].any()
+    assert torch.isfinite(ref.held(ack.t, 2, half, code)[1]).all()
+
+
 def test_relu_stops_infinite_gradients_and_nan_reads_back_as_nan(ctx):
     x, da = torch.full((1, 64), -1.0).cuda(), torch.full((1, 64), math.inf).cuda()
     x[0, 40] = math.nan
