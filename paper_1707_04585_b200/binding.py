@@ -139,10 +139,16 @@ def _stream():
 
 class Context:
     def __init__(self, device: int = 0):
-        global _types
+        global _types, _direct
         if not _types:
             import torch
             _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
+            lib()
+            try:
+                from . import _direct as module          # links to the library above
+                _direct = module
+            except ImportError:
+                pass
         self.h = C.c_void_p()
         self.device = device
         self.home = device if device >= 0 else -2        # where tensors have to be (a CPU tensor calls its place -1)
@@ -468,6 +474,9 @@ def _bad(what, name, why):
 
 _types = ()             # torch's types by revnet_dtype, then those of flat buffers; filled with the first context, so that importing this module needs no torch
 F32, BF16, I32, U8 = 0, 1, 2, 3
+# csrc/direct.cpp: the calls below, checks included, at a seventh of the host time.  It answers None where it finds anything wrong; then (and without
+# it) the code here checks, and says what.
+_direct = None
 
 
 def _strided(stride, rows, channels, ld):
@@ -536,24 +545,32 @@ def _a_channels(desc):
 
 
 def revnet_act_store(ctx, desc, x, ck, a=None):
+    if _direct and (rc := _direct.act_store(ctx.h.value, ctx.device, desc, x, ck, a)) is not None:
+        return ctx.check(rc, "revnet_act_store")
     w, rows, c = "revnet_act_store", desc.rows, desc.channels
     ctx.check(lib().revnet_act_store(ctx.h, desc, _row_ptr(ctx, w, "x", x, rows, c, desc.ld_x, desc.dtype), _ck_ptr(ctx, w, "ck", ck, rows, c),
                                      _row_ptr(ctx, w, "a", a, rows, _a_channels(desc), desc.ld_a, desc.dtype), _stream_of(ctx)), w)
 
 
 def revnet_act_load(ctx, desc, ck, a):
+    if _direct and (rc := _direct.act_load(ctx.h.value, ctx.device, desc, ck, a)) is not None:
+        return ctx.check(rc, "revnet_act_load")
     w, rows = "revnet_act_load", desc.rows
     ctx.check(lib().revnet_act_load(ctx.h, desc, _ck_ptr(ctx, w, "ck", ck, rows, desc.channels),
                                     _row_ptr(ctx, w, "a", a, rows, _a_channels(desc), desc.ld_a, desc.dtype), _stream_of(ctx)), w)
 
 
 def revnet_act_bwd(ctx, desc, ck, da, dx, a_ck=None):
+    if _direct and (rc := _direct.act_bwd(ctx.h.value, ctx.device, desc, ck, da, dx, a_ck)) is not None:
+        return ctx.check(rc, "revnet_act_bwd")
     w, rows, c, ca = "revnet_act_bwd", desc.rows, desc.channels, _a_channels(desc)
     ctx.check(lib().revnet_act_bwd(ctx.h, desc, _ck_ptr(ctx, w, "ck", ck, rows, c), _row_ptr(ctx, w, "da", da, rows, ca, desc.ld_a, desc.dtype),
                                    _row_ptr(ctx, w, "dx", dx, rows, c, desc.ld_x, desc.dtype), _ck_ptr(ctx, w, "a_ck", a_ck, rows, ca), _stream_of(ctx)), w)
 
 
 def revnet_rmsnorm_fwd(ctx, desc, x, r, gamma, h, n, ck, rstd):
+    if _direct and (rc := _direct.rmsnorm_fwd(ctx.h.value, ctx.device, desc, x, r, gamma, h, n, ck, rstd)) is not None:
+        return ctx.check(rc, "revnet_rmsnorm_fwd")
     w, rows, c, ls, lb, ts, tb = "revnet_rmsnorm_fwd", desc.rows, desc.channels, desc.ld_stream, desc.ld_branch, desc.stream_dtype, desc.branch_dtype
     ctx.check(lib().revnet_rmsnorm_fwd(
         ctx.h, desc, _row_ptr(ctx, w, "x", x, rows, c, ls, ts), _row_ptr(ctx, w, "r", r, rows, c, lb, tb), _flat_ptr(ctx, w, "gamma", gamma, c),
@@ -568,6 +585,8 @@ def revnet_rmsnorm_workspace_bytes(ctx, desc) -> int:
 
 
 def revnet_rmsnorm_bwd(ctx, desc, dn, dh, h, ck, rstd, gamma, dx, dr, dgamma, workspace):
+    if _direct and (rc := _direct.rmsnorm_bwd(ctx.h.value, ctx.device, desc, dn, dh, h, ck, rstd, gamma, dx, dr, dgamma, workspace)) is not None:
+        return ctx.check(rc, "revnet_rmsnorm_bwd")
     w, rows, c, ls, lb, ts, tb = "revnet_rmsnorm_bwd", desc.rows, desc.channels, desc.ld_stream, desc.ld_branch, desc.stream_dtype, desc.branch_dtype
     ws, size = _ws(ctx, w, workspace)
     ctx.check(lib().revnet_rmsnorm_bwd(
@@ -583,6 +602,8 @@ def revnet_linear_wgrad_workspace_bytes(ctx, desc) -> int:
 
 
 def revnet_linear_wgrad(ctx, desc, dy, ck, gamma, dW, workspace):
+    if _direct and (rc := _direct.linear_wgrad(ctx.h.value, ctx.device, desc, dy, ck, gamma, dW, workspace)) is not None:
+        return ctx.check(rc, "revnet_linear_wgrad")
     w, rows, ci, co = "revnet_linear_wgrad", desc.rows, desc.cin, desc.cout
     ws, size = _ws(ctx, w, workspace)
     ctx.check(lib().revnet_linear_wgrad(ctx.h, desc, _row_ptr(ctx, w, "dy", dy, rows, co, desc.ld_dy, desc.dy_dtype), _ck_ptr(ctx, w, "ck", ck, rows, ci),
@@ -590,6 +611,8 @@ def revnet_linear_wgrad(ctx, desc, dy, ck, gamma, dW, workspace):
 
 
 def revnet_logprobs_fwd(ctx, desc, logits, targets, logp, entropy, lse, top_logp=None, top_index=None):
+    if _direct and (rc := _direct.logprobs_fwd(ctx.h.value, ctx.device, desc, logits, targets, logp, entropy, lse, top_logp, top_index)) is not None:
+        return ctx.check(rc, "revnet_logprobs_fwd")
     w, rows = "revnet_logprobs_fwd", desc.rows
     ctx.check(lib().revnet_logprobs_fwd(
         ctx.h, desc, _row_ptr(ctx, w, "logits", logits, rows, desc.vocab, desc.ld, desc.dtype), _flat_ptr(ctx, w, "targets", targets, rows, I32),
@@ -598,6 +621,8 @@ def revnet_logprobs_fwd(ctx, desc, logits, targets, logp, entropy, lse, top_logp
 
 
 def revnet_logprobs_bwd(ctx, desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits):
+    if _direct and (rc := _direct.logprobs_bwd(ctx.h.value, ctx.device, desc, logits, targets, lse, entropy, dlogp, dentropy, dlogits)) is not None:
+        return ctx.check(rc, "revnet_logprobs_bwd")
     w, rows = "revnet_logprobs_bwd", desc.rows
     ctx.check(lib().revnet_logprobs_bwd(
         ctx.h, desc, _row_ptr(ctx, w, "logits", logits, rows, desc.vocab, desc.ld, desc.dtype), _flat_ptr(ctx, w, "targets", targets, rows, I32),

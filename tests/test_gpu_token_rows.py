@@ -776,3 +776,68 @@ def test_refusals_on_the_device(ctx):
     with pytest.raises(B.RevnetError) as e:
         B.revnet_linear_wgrad(ctx, d, x, ck.t, None, torch.empty(64, 64, device="cuda"), torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == -3
+
+
+# ------------------------------------------------------------------ calls that skip ctypes
+def every_call(ctx):
+    """One call of each entry point -> what they wrote."""
+    rows, c = 9, 64
+    x, r, dn = (data(rows, c, "f32", i).cuda() for i in (41, 42, 43))
+    gamma, rstd, dg = torch.ones(c, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(c, device="cuda")
+    h, n, dx, dr, a, da = (torch.zeros(rows, c, device="cuda") for _ in range(6))
+    ck, ack = Ck(rows, c), Ck(rows, c)
+    d = B.norm_desc(rows, c, "f32", "f32")
+    ws = torch.zeros(B.revnet_rmsnorm_workspace_bytes(ctx, d), dtype=torch.uint8, device="cuda")
+    B.revnet_rmsnorm_fwd(ctx, d, x, r, gamma, h, n, ck.t, rstd)
+    B.revnet_rmsnorm_bwd(ctx, d, dn, None, None, ck.t, rstd, gamma, dx, dr, dg, ws)
+    e = B.act_desc(rows, c, "f32", act="silu")
+    B.revnet_act_load(ctx, e, ck.t, a)
+    B.revnet_act_bwd(ctx, e, ck.t, dn, da, ack.t)
+    dW, kept = torch.empty(c, c, device="cuda"), Ck(rows, c)
+    B.revnet_act_store(ctx, e, x, kept.t)
+    f = B.wgrad_desc(rows, c, c, "f32")
+    ws2 = torch.zeros(B.revnet_linear_wgrad_workspace_bytes(ctx, f), dtype=torch.uint8, device="cuda")
+    B.revnet_linear_wgrad(ctx, f, dn, kept.t, None, dW, ws2)
+    g = B.logprob_desc(rows, c, "f32", 3)
+    logp, entropy, lse = (torch.empty(rows, device="cuda") for _ in range(3))
+    top, index, targets, dl = torch.empty(rows, 3, device="cuda"), torch.empty(rows, 3, dtype=torch.int32, device="cuda"), torch.arange(rows, dtype=torch.int32, device="cuda"), torch.empty_like(x)
+    B.revnet_logprobs_fwd(ctx, g, x, targets, logp, entropy, lse, top, index)
+    B.revnet_logprobs_bwd(ctx, g, x, targets, lse, entropy, logp, None, dl)
+    return [h, n, rstd, dx, dr, dg, a, da, dW, ack.t, kept.t, logp, entropy, lse, top, index, dl]
+
+
+def test_direct_calls_do_what_the_checked_ones_do(ctx, monkeypatch):
+    assert B._direct is not None
+    with monkeypatch.context() as m:
+        m.setattr(B, "_direct", None)
+        want = every_call(ctx)
+
+    def unused(*a):
+        raise AssertionError("the direct call was not taken")
+    for name in ("_row_ptr", "_flat_ptr", "_ck_ptr", "_ws", "_stream_of"):
+        monkeypatch.setattr(B, name, unused)
+    assert all(torch.equal(a, b) for a, b in zip(every_call(ctx), want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):     # on the stream that is current
+        got = every_call(ctx)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_direct_calls_leave_refusals_to_the_checked_ones(ctx):
+    d, x, ck = B.act_desc(4, 64, "f32"), torch.zeros(4, 64, device="cuda"), Ck(4, 64)
+    call = lambda *a: B._direct.act_store(ctx.h.value, ctx.device, *a)
+    assert call(d, x, ck.t, None) == 0
+    for bad in (x[:, :63], x.double(), x.cpu(), x.t(), x.bfloat16(), x[:3], x.view(-1), x.to_sparse(), "x", 5, x.expand(2, 4, 64)):
+        assert call(d, bad, ck.t, None) is None
+    assert call(d, x, ck.t[:-1], None) is None and call(d, x, ck.t.to(torch.int8), None) is None and call(d, x, ck.t) is None
+    assert call(B.logprob_desc(4, 64, "f32"), x, ck.t, None) is None and call(None, x, ck.t, None) is None
+    assert B._direct.act_store(0, ctx.device, d, x, ck.t, None) is None and B._direct.act_store(ctx.h.value, ctx.device + 1, d, x, ck.t, None) is None
+    assert B._direct.act_store(None, ctx.device, d, x, ck.t, None) is None
+    with pytest.raises(B.RevnetError, match="x must be"):
+        B.revnet_act_store(ctx, d, x.double(), ck.t)
+    with pytest.raises(B.RevnetError) as e:              # what only the entry point refuses
+        B.revnet_act_store(ctx, B.act_desc(4, 63, "f32", act="swiglu"), torch.zeros(4, 63, device="cuda"), Ck(4, 63).t)
+    assert e.value.status < 0
+    torch.cuda.synchronize()
