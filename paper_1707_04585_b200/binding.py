@@ -474,8 +474,8 @@ def _bad(what, name, why):
 
 _types = ()             # torch's types by revnet_dtype, then those of flat buffers; filled with the first context, so that importing this module needs no torch
 F32, BF16, I32, U8 = 0, 1, 2, 3
-# csrc/direct.cpp: the calls below, checks included, at a seventh of the host time.  It answers None where it finds anything wrong; then (and without
-# it) the code here checks, and says what.
+# csrc/direct.cpp: the calls below, checks included, at less than half of the host time.  It answers None where it finds anything wrong; then (and
+# without it) the code here checks, and says what.
 _direct = None
 
 

@@ -1,6 +1,7 @@
-// Calls from Python to the operators on rows of tokens without ctypes: binding.py checks seven tensors in 4 us and marshals a call in 1.5, where a
-// small kernel's launch takes 4.  A call here does the same checks in well under a microsecond.  It answers the entry point's status, or None
-// where anything is not as it has to be: binding.py then checks again, attribute by attribute, and says what is wrong.
+// Calls from Python to the operators on rows of tokens without ctypes.  Small ones are bound by the host: the forward norm of 1 x 4096 takes 6.6 us of
+// it when binding.py checks its seven tensors and marshals the call, 2.8 here, launch included (loading 1 x 4096 from 8 bits: 4.3 and 2.5).  The checks
+// are the same.  A call answers the entry point's status, or None where anything is not as it has to be: binding.py then checks again, attribute
+// by attribute, and says what is wrong.
 #include <Python.h>
 #include <cstring>
 #include <ATen/core/Tensor.h>
