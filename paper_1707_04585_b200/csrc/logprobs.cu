@@ -32,22 +32,36 @@ struct LogpArgs {
     int *status;
 };
 
-// a row's running sums: m the maximum (in units of log 2: y = x log2 e), s = sum 2^(y - m), t = sum (y - m) 2^(y - m)
+// A row's running sums: m the maximum, s = sum 2^d, t = sum d 2^d with d a logit's distance from the maximum in units of log 2.
+// Up to kFar in magnitude d is one fused operation, x log2 e - M with M = m log2 e rounded: what the rounding takes, at most 1/16, s gains.  Beyond,
+// it would grow past what 2^d holds (at 5e9 it is 220) and M overflow, so there d = (x - m) log2 e, exact where it is small.  m is kept as M / 2 below
+// kFar and as the logit itself beyond: so the value tells which it is, and the order is the logits'.
 struct Sums { float m, s, t; };
+constexpr float kFar = 1048576.f;
+__device__ __forceinline__ bool far(float m) { return fabsf(m) > kFar; }         // (-inf, of no logit yet, among them)
+__device__ __forceinline__ float level(float x) { return far(x) ? x : x * (0.5f * kLog2e); }
+__device__ __forceinline__ float distance(float a, float b) {                    // from level b to a
+    if (far(a)) return far(b) ? (a - b) * kLog2e : fmaf(a, kLog2e, -2.f * b);
+    return far(b) ? fmaf(-b, kLog2e, 2.f * a) : 2.f * (a - b);
+}
 // a's sums as they are for the maximum m >= a.m; an empty or all -inf one (m = -inf) is zero for any m
 __device__ __forceinline__ void rescale(Sums &a, float m) {
     if (a.m == -INFINITY || a.m == m) { a.m = m; return; }
-    const float d = a.m - m, e = exp2_ftz(d);
+    const float d = distance(a.m, m), e = exp2_ftz(d);
     a.t = (a.t + d * a.s) * e;
     a.s *= e;
-    if (e == 0.f) a.t = 0.f;         // d = -inf: m is +inf, and the row's sums are NaN through its own element
+    if (e == 0.f) a.t = 0.f;         // d may be -inf (m +inf: the row's sums are NaN through its own element)
     a.m = m;
 }
-__device__ __forceinline__ Sums join(Sums a, Sums b) {
-    const float m = fmaxf(a.m, b.m);
+// the warp's sums, in every lane
+__device__ __forceinline__ Sums join(Sums a) {
+    float m = a.m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     rescale(a, m);
-    rescale(b, m);
-    return Sums{m, a.s + b.s, a.t + b.t};
+#pragma unroll
+    for (int o = 16; o; o >>= 1) { a.s += __shfl_xor_sync(0xffffffffu, a.s, o); a.t += __shfl_xor_sync(0xffffffffu, a.t, o); }
+    return a;
 }
 // two float32 operations in one instruction
 typedef unsigned long long f32x2;
@@ -59,10 +73,19 @@ __device__ __forceinline__ float both(f32x2 v) { float lo, hi; parts(v, lo, hi);
 
 // N logits, N a multiple of 4 or 1, top the largest of them
 template <int N> __device__ __forceinline__ void add(Sums &a, const float (&x)[N], float top) {
-    top *= kLog2e;
+    top = level(top);
     if (top > a.m) rescale(a, top);
-    // (a.m stays -inf while every logit so far is: then all differences would be NaN)
-    const float m = a.m == -INFINITY ? 0.f : a.m;
+    if (far(a.m)) {                  // one logit at a time; -inf adds nothing, also where there is nothing else yet
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if (x[i] == -INFINITY) continue;
+            const float d = (x[i] - a.m) * kLog2e, e = exp2_ftz(d);
+            a.s += e;
+            a.t = fmaf(fmaxf(d, -200.f), e, a.t);                // (0 log 0 = 0)
+        }
+        return;
+    }
+    const float m = 2.f * a.m;
     float s, t;
     if constexpr (N == 1) {
         const float d = fmaf(x[0], kLog2e, -m);
@@ -180,9 +203,9 @@ template <class T> __device__ __forceinline__ T remote(const T *p, uint32_t rank
     return v;
 }
 
-// not above 0, which rounding could otherwise reach
-__device__ __forceinline__ float log_prob(float x, double lse, bool none) {
-    const float v = (float)((double)x - lse);
+// x - base - logs, not above 0, which rounding could otherwise reach; beside a base of 1e38 the sum base + logs has no room for logs
+__device__ __forceinline__ float log_prob(float x, double base, double logs, bool none) {
+    const float v = (float)(((double)x - base) - logs);
     return none ? -INFINITY : (v > 0.f ? 0.f : v);
 }
 
@@ -267,10 +290,7 @@ __global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) 
         if (ok) add(sum, f, f[0]);
         if constexpr (TOP) list.offer(ok ? key_of(f[0], begin + i) : 0ull);
     }
-    for (int o = 16; o; o >>= 1) {
-        const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
-        sum = join(sum, b);
-    }
+    sum = join(sum);
     if (lane == 0) { sm_m[warp] = sum.m; sm_s[warp] = sum.s; sm_t[warp] = sum.t; }
     if constexpr (TOP) lists[warp * 32 + lane] = list.mine;
     __syncthreads();
@@ -282,20 +302,14 @@ __global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) 
     if (warp == 0) {
         // lane w: the sums of warp w
         sum = lane < warps ? Sums{sm_m[lane], sm_s[lane], sm_t[lane]} : Sums{-INFINITY, 0.f, 0.f};
-        for (int o = 16; o; o >>= 1) {
-            const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
-            sum = join(sum, b);
-        }
+        sum = join(sum);
         if (CLUSTER && lane == 0) { sm_m[0] = sum.m; sm_s[0] = sum.s; sm_t[0] = sum.t; }
     }
     if (CLUSTER) {
         cluster_sync();
         if (rank == 0 && warp == 0) {
             sum = lane < (int)ctas ? Sums{remote(&sm_m[0], lane), remote(&sm_s[0], lane), remote(&sm_t[0], lane)} : Sums{-INFINITY, 0.f, 0.f};
-            for (int o = 16; o; o >>= 1) {
-                const Sums b{__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), __shfl_xor_sync(0xffffffffu, sum.t, o)};
-                sum = join(sum, b);
-            }
+            sum = join(sum);
             if constexpr (TOP) {
                 Key others[8];
 #pragma unroll
@@ -309,16 +323,16 @@ __global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) 
         if (rank != 0) return;
     }
     if (warp != 0) return;
-    // once per row, in double: y = x kLog2e with the float kLog2e, so m / kLog2e is the largest logit without the rounding of m, which s makes up for
+    // once per row, in double.  The level stands for M / log2 e, with the float kLog2e that M was formed with, not quite the largest logit: s makes up for that
     const bool none = sum.m == -INFINITY && sum.s == 0.f;
-    const double logs = (double)logf(sum.s), lse = none ? (double)-INFINITY : (double)sum.m / (double)kLog2e + logs;
+    const double logs = (double)logf(sum.s), base = far(sum.m) ? (double)sum.m : 2.0 * sum.m / (double)kLog2e;
     if (lane == 0) {
-        if (p.lse) p.lse[row] = (float)lse;
+        if (p.lse) p.lse[row] = none ? -INFINITY : (float)(base + logs);
         if (p.ent) { const float h = (float)(logs - (double)kLn2 * ((double)sum.t / sum.s)); p.ent[row] = none || h < 0.f ? 0.f : h; }
         if (p.logp) {
             const int tgt = p.targets[row];
             float v = 0.f;
-            if (tgt >= 0 && tgt < p.vocab) v = log_prob(to_f(x[tgt]), lse, none);
+            if (tgt >= 0 && tgt < p.vocab) v = log_prob(to_f(x[tgt]), base, logs, none);
             else if (tgt != -1) { v = NAN; atomicExch(p.status, (int)REVNET_E_INVALID_ARG); }
             p.logp[row] = v;
         }
@@ -326,7 +340,7 @@ __global__ void __launch_bounds__(512, 2) logprobs_fwd_kernel(const LogpArgs p) 
     if constexpr (TOP)
         if (lane < p.k) {
             p.top_index[row * p.k + lane] = (int)~(uint32_t)list.mine;
-            p.top_logp[row * p.k + lane] = log_prob(value_of(list.mine), lse, none);
+            p.top_logp[row * p.k + lane] = log_prob(value_of(list.mine), base, logs, none);
         }
 }
 

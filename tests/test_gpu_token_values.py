@@ -1,0 +1,111 @@
+"""Operators on rows of tokens at values where float32's range or resolution ends, against float64.  Tolerances are bounds on rounding errors, as in
+test_gpu_token_rows.py."""
+import math
+
+import pytest
+import torch
+
+from paper_1707_04585_b200 import binding as B
+from tests import token_ref as ref
+from tests.test_gpu_token_rows import Ck, Rows, data, wgrad, within
+from tests.token_ref import DT, U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Context(0)
+    yield c
+    B.revnet_check_device(c)
+    c.close()
+
+
+# ------------------------------------------------------------------ log probabilities of large finite logits
+def large_logits(vocab, dtype, seed=1):
+    """Rows by name: masks of the type's lowest value and of round numbers, the largest values, and values whose differences are small beside them."""
+    g = torch.Generator().manual_seed(seed)
+    lo, hi = torch.finfo(DT[dtype]).min, torch.finfo(DT[dtype]).max
+
+    def normal():
+        return torch.randn(vocab, generator=g) * 3
+
+    def full(v):
+        return torch.full((vocab,), float(v))
+
+    def mixed(*parts):               # the parts' values by turns
+        t = torch.stack([p if torch.is_tensor(p) else full(p) for p in parts])
+        return t[torch.arange(vocab) % len(parts), torch.arange(vocab)]
+
+    def with_one(t, v, at=None):
+        t = t.clone()
+        t[vocab // 3 if at is None else at] = v
+        return t
+    near = torch.rand(vocab, generator=g) * 4 - 2
+    rows = dict(all_lowest=full(lo), all_largest=full(hi), half_lowest=mixed(lo, normal()), lowest_and_none=mixed(lo, -math.inf), one_left=with_one(full(lo), -3.0),
+                one_large=with_one(normal(), 2.5e38), one_largest=with_one(normal(), hi, vocab - 1), two_large=with_one(with_one(normal(), 3e38), 3e38, 0),
+                all_5e9=full(-5e9), all_1e10=full(1e10), masked_1e10=mixed(-1e10, normal(), normal()), all_masks=mixed(-1e9, -1e10, lo), all_1e30=full(-1e30), both_signs=mixed(-1e30, 1e30),
+                around_million=near + 2.0 ** 20, around_minus_million=near - 2.0 ** 20, thousands=near - 3000.0, growing=torch.linspace(-88, 88, vocab).double().exp().float() * 4,
+                shrinking=-torch.linspace(-88, 88, vocab).double().exp().float().flip(0) * 4, falling=torch.linspace(88, -88, vocab).double().exp().float() * 4,       # (to +inf: NaN)
+                growing_finite=torch.linspace(-88, 88, vocab).double().exp().float() * 2, falling_finite=torch.linspace(88, -88, vocab).double().exp().float() * 2)
+    return list(rows), torch.stack(list(rows.values())).to(DT[dtype])
+
+
+def definition(x, targets):
+    """Float64 -> (lse, logp of the targets, entropy, log p of every logit): in differences from the maximum, since lse alone has no room for log s beside 1e38."""
+    m = x.amax(1, keepdim=True)
+    logs = torch.log(torch.exp(x - m).sum(1, keepdim=True))
+    q = (x - m) - logs
+    p = torch.exp(q)
+    ent = -torch.where(p == 0, 0.0, p * q).sum(1)
+    return (m + logs)[:, 0], torch.where(targets < 0, 0.0, q.gather(1, targets.clamp_min(0).long()[:, None])[:, 0]), ent, q
+
+
+def forward(ctx, r, targets, vocab, dtype, k):
+    n = r.t.shape[0]
+    out = [torch.empty(n, device="cuda") for _ in range(3)]
+    tl = torch.empty(n, k, device="cuda") if k else None
+    ti = torch.empty(n, k, dtype=torch.int32, device="cuda") if k else None
+    B.revnet_logprobs_fwd(ctx, B.logprob_desc(n, vocab, dtype, k, r.ld), r.t, targets.cuda(), *out, tl, ti)
+    return out, tl, ti
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,pad,repeat", [(5, 0, 1), (1000, 0, 1), (1003, 3, 1), (40000, 0, 1), (4099, 0, 60), (131072, 0, 0)])
+def test_log_probabilities_of_large_logits(ctx, vocab, pad, repeat, dtype):
+    """One row per CTA, rows cut over a cluster (few of them), a single row at a time."""
+    names, x = large_logits(vocab, dtype)
+    g = torch.Generator().manual_seed(vocab)
+    targets = torch.randint(0, vocab, (len(names),), generator=g, dtype=torch.int32)
+    targets[names.index("one_large")] = vocab // 3
+    lse, logp, ent, q = definition(x.double(), targets)
+    # exponents (x - m) log2 e are off by 2 * 2^-24 of themselves, and beyond 32 of them the weight is below 2^-32; ex2 by 2^-22; logs and last roundings
+    tol = 64 * 2.0 ** -24 + 2.0 ** -21
+    for rows in [slice(i, i + 1) for i in range(len(names))] if repeat == 0 else [slice(None)]:
+        n = max(repeat, 1)
+        xs, ts = x[rows].repeat(n, 1), targets[rows].repeat(n)
+        r = Rows(xs.shape[0], vocab, dtype, pad, 0, xs)
+        for k in (0, min(5, vocab)):
+            out, tl, ti = forward(ctx, r, ts, vocab, dtype, k)
+            within(out[0].cpu().double(), logp[rows].repeat(n), tol * torch.ones(xs.shape[0], dtype=torch.float64))
+            within(out[1].cpu().double(), ent[rows].repeat(n), 2 * tol * (1 + ent[rows].repeat(n)))
+            within(out[2].cpu().double(), lse[rows].repeat(n), tol * torch.ones(xs.shape[0], dtype=torch.float64))
+            if k:
+                want = ref.top(x[rows].double(), k)
+                assert torch.equal(ti.cpu(), want.repeat(n, 1))
+                within(tl.cpu().double(), q[rows].gather(1, want.long()).repeat(n, 1), torch.full((xs.shape[0], k), tol, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("vocab", [40, 3000, 70000])
+def test_bad_logits_among_large_ones_stay_bad(ctx, vocab):
+    x = torch.full((6, vocab), torch.finfo(torch.float32).min)
+    x[0, 7], x[1, vocab - 1], x[2] = math.nan, math.inf, -math.inf
+    x[3], x[3, 2] = -math.inf, math.nan
+    x[4], x[4, 5] = torch.finfo(torch.float32).max, math.nan
+    x[5], x[5, 9] = torch.finfo(torch.float32).max, math.inf
+    out, tl, ti = forward(ctx, Rows(6, vocab, "f32", value=x), torch.zeros(6, dtype=torch.int32), vocab, "f32", 3)
+    bad = torch.tensor([True, True, False, True, True, True])
+    for o in out:
+        assert torch.isnan(o.cpu()[bad]).all()
+    assert out[0][2] == -math.inf and out[1][2] == 0 and out[2][2] == -math.inf and (tl[2] == -math.inf).all()
+    assert torch.equal(ti.cpu(), ref.top(x.double(), 3))
