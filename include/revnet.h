@@ -422,7 +422,9 @@ int revnet_logprobs_fwd(revnet_ctx *ctx, const revnet_logprob_desc *desc, const 
                         float *logp, float *entropy, float *lse, float *top_logp, int32_t *top_index, void *stream);
 /* dlogits_j = dlogp (1[j = target] - p_j) - dentropy p_j (log p_j + entropy), 0 where p_j = 0 and j is not the target.
  * dlogp (with targets) or dentropy (with entropy) may be null: 0.  dlogits == logits is legal.  A target outside [-1, vocab) makes its
- * row NaN (where p > 0) and sets the device status.  A row whose lse is -inf gets zeros. */
+ * row NaN (where p > 0) and sets the device status.  A row whose lse is -inf gets zeros.
+ * lse may be that of more logits than the call sees (parts of a vocabulary).  Where |lse| > 4096 float32 has no room for its last digits (all logits
+ * -1e9: lse = -1e9 whatever their number): such a row is summed again, and its own lse taken in full, if the given one is that to float32's step. */
 int revnet_logprobs_bwd(revnet_ctx *ctx, const revnet_logprob_desc *desc, const void *logits, const int32_t *targets,
                         const float *lse, const float *entropy, const float *dlogp, const float *dentropy, void *dlogits, void *stream);
 

@@ -109,3 +109,61 @@ def test_bad_logits_among_large_ones_stay_bad(ctx, vocab):
         assert torch.isnan(o.cpu()[bad]).all()
     assert out[0][2] == -math.inf and out[1][2] == 0 and out[2][2] == -math.inf and (tl[2] == -math.inf).all()
     assert torch.equal(ti.cpu(), ref.top(x.double(), 3))
+
+
+def gradient(ctx, r, targets, lse, ent, gl, ge, out):
+    n, vocab = r.t.shape
+    dtype = "f32" if r.t.dtype == torch.float32 else "bf16"
+    B.revnet_logprobs_bwd(ctx, B.logprob_desc(n, vocab, dtype, 0, r.ld), r.t, targets.cuda(), lse, ent, gl.cuda(), ge.cuda() if ge is not None else None, out.t)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,pad,repeat", [(5, 0, 1), (1000, 0, 1), (1003, 3, 1), (70000, 0, 1), (4099, 0, 60), (200000, 0, 1)])
+def test_gradient_of_large_logits(ctx, vocab, pad, repeat, dtype):
+    """From the lse and entropy that the forward call gave, which float32 holds to 2^-24 of lse only: rows where that is coarse are summed again."""
+    names, x = large_logits(vocab, dtype)
+    keep = torch.isfinite(x.double().amax(1))                    # (rows with +inf are NaN)
+    x = x[keep].repeat(repeat, 1)
+    n = x.shape[0]
+    g = torch.Generator().manual_seed(vocab + 1)
+    targets = torch.randint(-1, vocab, (n,), generator=g, dtype=torch.int32)
+    gl, ge = torch.randn(n, generator=g), torch.randn(n, generator=g)
+    r = Rows(n, vocab, dtype, pad, 0, x)
+    (logp, ent, lse), _, _ = forward(ctx, r, targets, vocab, dtype, 0)
+    lse64, _, ent64, q = definition(x.double(), targets)
+    p = torch.exp(q)
+    live = torch.where(targets < 0, 0.0, gl.double())[:, None]
+    hot = torch.zeros_like(q).scatter_(1, targets.clamp_min(0).long()[:, None], 1.0) * live
+    for b in (None, ge):
+        w = b.double()[:, None] if b is not None else 0.0
+        bent = torch.where(p > 0, q + ent64[:, None], 0.0)
+        want = hot - p * (live + w * bent)
+        size = p * (live.abs() + (w.abs() if b is not None else 0.0) * torch.where(p > 0, q.abs() + ent64[:, None], 0.0))
+        # q is off by what float32 keeps of lse (up to 4096; beyond, log s is kept apart), by 3 * 2^-24 of itself (the difference, the factor, its product) and
+        # by log s's 2^-21; ex2 by 2^-22; the entropy by the forward's tolerance; a few roundings
+        dq = 3 * U * q.abs() + U * lse64.abs().clamp_max(4096)[:, None] + 2.0 ** -20
+        dent = ((64 * 2.0 ** -24 + 2.0 ** -21) * 2 * (1 + ent64) + U * ent64)[:, None]
+        tol = torch.where(p > 0, size * dq + p * (w.abs() if b is not None else 0.0) * (dq + dent) + 8 * U * size, 0.0) + 2.0 ** -126 * (1 + live.abs() + 200 * (w.abs() if b is not None else 0.0)) + 2 * U * hot.abs()
+        out = Rows(n, vocab, dtype, pad)
+        gradient(ctx, r, targets, lse, ent if b is not None else None, gl, b, out)
+        within(out.cpu(), want, tol, dtype)
+        assert out.untouched()
+        again = Rows(n, vocab, dtype, pad, 0, x)                 # in place: every part of a row has to see all of it before any is overwritten
+        gradient(ctx, again, targets, lse, ent if b is not None else None, gl, b, again)
+        assert torch.equal(again.t, out.t) and again.untouched()
+
+
+@pytest.mark.parametrize("size,vocab", [(1e4, 3000), (1e6, 50000)])
+def test_gradient_of_a_part_of_a_vocabulary_takes_the_given_lse(ctx, size, vocab):
+    """lse of more logits than the call sees: it is taken as it is, however coarse."""
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(4, vocab, generator=g) + size
+    rest = torch.full((4, 1), float(size + 20 * max(1.0, size * 2.0 ** -20)))      # one more logit, far above
+    lse = torch.logsumexp(torch.cat([x, rest], 1).double(), 1).float()
+    targets, gl = torch.tensor([0, 5, -1, vocab - 1], dtype=torch.int32), torch.randn(4, generator=g)
+    r, out = Rows(4, vocab, "f32", value=x), Rows(4, vocab, "f32")
+    gradient(ctx, r, targets, lse.cuda(), None, gl, None, out)
+    want = ref.logprobs_bwd(x.double(), targets, lse.double(), torch.zeros(4, dtype=torch.float64), gl.double(), torch.zeros(4, dtype=torch.float64))
+    q = x.double() - lse.double()[:, None]
+    hot = torch.zeros_like(want).scatter_(1, targets.clamp_min(0).long()[:, None], 1.0) * gl.double().abs()[:, None]
+    within(out.cpu(), want, torch.exp(q) * gl.double().abs()[:, None] * (3 * U * q.abs() + 2.0 ** -20) + 2.0 ** -126 + 2 * U * hot)
