@@ -389,7 +389,7 @@ int revnet_rmsnorm_bwd(revnet_ctx *ctx, const revnet_norm_desc *desc, const void
 /* Weight gradient of a linear layer (a 1x1 convolution) whose input was kept in 8 bits:
  *   dW[o][c] = gamma[c] * sum over rows t of dy[t][o] * x8[t][c],   dW [cout][cin] float32, overwritten
  * on the tensor cores.  Products are exact: x8 and a bf16 dy are bf16 operands; a float32 dy is split into three bf16 numbers that
- * together hold all its 24 bits (three products).  gamma null: ones.  Sums are kept in float32, rounded to nearest at least every 2048
+ * together hold all its 24 bits (three products).  gamma null: ones.  Sums are kept in float32, rounded to nearest at least every 1024
  * rows.  bf16 rows a multiple of 16 bytes apart are read from where they are and must start on 16 bytes (REVNET_E_MISALIGNED); any other
  * dy is laid out in the workspace first. */
 typedef struct {

@@ -7,9 +7,11 @@
 //   codes  TMA -> shared memory (64 rows x 128 channels) -> twelve decoder warps -> bf16 in the same swizzled layout: the B operand
 //   D      256 output channels x 256 input channels of fp32 in the pair's tensor memory, twice
 //
-// Long sums: the tensor cores round their running sum towards zero, an error that grows with the number of rows (7.8e-6 relative after about
-// 10000).  So a run of MMAs covers 2048 rows; eight warps of their own then add its result to sums in registers (128 per thread), to
-// nearest, while the MMAs of the next run fill the other half of tensor memory: 5e-7 for any number of rows.
+// Long sums: the tensor cores round their running sum towards zero, an error that grows with the number of rows (operands of mean zero: 7.8e-6
+// relative after about 10000) and is a bias where the operands have one sign.  So a run of MMAs covers 1024 rows; eight warps of their own then
+// add its result to sums in registers (128 per thread), to nearest, while the MMAs of the next run fill the other half of tensor memory.  Relative
+// error of 512 x 512 from 65536 rows, mean zero and one sign, by rows per run: 2048 4.3e-7 and 1.9e-6, 1024 2.2e-7 and 8e-7, 512 1.4e-7 and
+// 3.2e-7, 256 1.2e-7 and 1.3e-7 (a sum in float32 throughout: 2e-7 and 1.7e-7); 16384 rows, 4096 x 4096: 346, 350, 364, 379 us.
 //
 // Decoding has to keep up with 512 clocks of MMAs per 64 x 128 codes, about 850 warp instructions.  What it took, 16384 rows, 4096 x 4096:
 // 854 us with eight warps that reported every step at cluster scope, 740 at CTA scope, 557 with steps dealt out to groups of warps so that
@@ -33,7 +35,7 @@ constexpr int kGroups = 6, kGroupWarps = kDecoders / kGroups;    // every kGroup
 constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
 static_assert((4 + kDecoders) * kRegsFew + kSummers * kRegsSums == kThreads / 32 * kRegs, "the split is the launch's total");
 constexpr int kStep = 64;            // rows per step
-constexpr int kRun = 32;             // steps per run of the tensor cores' own sum
+constexpr int kRun = 16;            // steps per run of the tensor cores' own sum
 constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
 constexpr int kMaxPairs = 80;
 constexpr int kStepsMin = 8;         // a pair's share of a tile is at least that long: shorter ones do not pay for their sums

@@ -167,3 +167,78 @@ def test_gradient_of_a_part_of_a_vocabulary_takes_the_given_lse(ctx, size, vocab
     q = x.double() - lse.double()[:, None]
     hot = torch.zeros_like(want).scatter_(1, targets.clamp_min(0).long()[:, None], 1.0) * gl.double().abs()[:, None]
     within(out.cpu(), want, torch.exp(q) * gl.double().abs()[:, None] * (3 * U * q.abs() + 2.0 ** -20) + 2.0 ** -126 + 2 * U * hot)
+
+
+# ------------------------------------------------------------------ weight gradients over many rows
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cin,cout", [(1000, 96, 136), (2048, 4096, 4096), (16500, 2048, 1280), (66000, 1530, 1790)])
+def test_weight_gradient_of_many_rows_of_one_sign(ctx, rows, cin, cout, dtype):
+    """The tensor cores cut their running sum off after every 16 rows.  With operands of one sign that is a bias, half a step of 2^-23 on average; a run of
+    1024 rows has 64 of them, of a sum that is half the run's on average, whatever the number of runs.  (Tiles enough for shares of several runs.)"""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cin, device="cuda", generator=g).abs()
+    dy = torch.randn(rows, cout, device="cuda", generator=g).abs().to(DT[dtype])
+    ck, x8 = Ck(rows, cin), torch.empty(rows, cin, device="cuda")
+    B.revnet_act_store(ctx, B.act_desc(rows, cin, "f32"), x, ck.t)
+    B.revnet_act_load(ctx, B.act_desc(rows, cin, "f32"), ck.t, x8)
+    got = wgrad(ctx, Rows(rows, cout, dtype, value=dy), ck, cin, None, "int8", dtype).cuda()
+    want = dy.double().T @ x8.double()
+    err = (got - want) / want
+    assert abs(err.mean()) <= 64 / 2 / 2 * 2.0 ** -23
+    # at most two steps each time, and a rounding per run and part
+    assert err.abs().max() <= 64 / 2 * 2.0 ** -22 + (rows / 1024 + 80) * U
+
+
+def schedule(rows, cin, cout, parts, sms):
+    """How the kernel deals out its tiles (csrc/wgrad8.cu): whole tiles per pair, tiles left over, pairs that share those, whether a pair's share goes on from one
+    tile into the next."""
+    steps, most = -(-rows // 64) * parts, min(sms // 2, 80)
+    tiles = -(-cin // 256) * -(-cout // 256)
+
+    def sharers_of(t):
+        return min(max(t, -(-t * steps // 8)), most)
+    pairs = sharers_of(tiles)
+    if tiles < pairs and steps - tiles * steps // pairs < 32:
+        pairs = tiles
+    waves = tiles // pairs
+    rest = tiles - waves * pairs
+    sharers = sharers_of(rest) if rest else 0
+    if rest and steps - rest * steps // sharers < 32:
+        sharers = rest
+    elif rest and sharers // rest * rest >= sharers * 85 // 100:
+        sharers -= sharers % rest
+    begin = [rest * steps * q // sharers for q in range(sharers + 1)] if sharers else []
+    crossing = any(a // steps != (b - 1) // steps for a, b in zip(begin, begin[1:]))
+    split = rest > 0 and rest % sharers != 0
+    return waves, rest, sharers, crossing, split
+
+
+# rows, input and output channels; whole tiles per pair, whether tiles are cut, whether a share crosses from one into the next (148 SMs)
+SCHEDULES = [(4096, 1280, 1024, 0, True, True), (8192, 2560, 1000, 0, True, True), (4096, 4096, 4096, 3, True, False), (4096, 500, 12032, 1, True, True),
+             (8100, 1530, 4860, 1, True, True), (64, 4096, 5120, 4, False, False), (100, 2049, 10000, 4, False, False)]
+
+
+@pytest.mark.parametrize("dtype,code", [("bf16", "int8"), ("bf16", "e4m3"), ("f32", "int8")])
+@pytest.mark.parametrize("rows,cin,cout,waves,cut,crossing", SCHEDULES)
+def test_weight_gradient_schedules(ctx, rows, cin, cout, waves, cut, crossing, dtype, code):
+    """Pairs with several whole tiles, tiles cut into parts behind them, shares that cross from one tile into the next."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    if dtype == "f32":
+        rows = rows // 3             # (three products: about the same schedule)
+    got_waves, rest, sharers, got_crossing, got_cut = schedule(rows, cin, cout, 3 if dtype == "f32" else 1, sms)
+    if sms == 148 and dtype == "bf16":
+        assert (got_waves, got_cut, got_crossing) == (waves, cut, crossing)
+    ld = -(-cout // 8) * 8
+    d = B.wgrad_desc(rows, cin, cout, dtype, code, ld)
+    prepared = 0 if dtype == "bf16" else -(-(-(-rows // 64) * 3 * 64 * ld * 2) // 256) * 256
+    assert B.revnet_linear_wgrad_workspace_bytes(ctx, d) == prepared + (sharers * 2 * 65536 * 4 if got_cut else 0) + 256
+    x, dy = data(rows, cin, "f32", 23), data(rows, cout, dtype, 24)
+    ck = Ck.of(x.double(), code, fill=0xFF)
+    rdy = Rows(rows, cout, dtype, ld - cout, 0, dy)
+    got = wgrad(ctx, rdy, ck, cin, None, code, dtype).cuda()
+    x8, dy64 = ref.held(ck.t, rows, cin, code).cuda(), dy.double().cuda()
+    want, size = dy64.T @ x8, dy64.abs().T @ x8.abs()
+    # as in test_weight_gradient, runs of 1024 rows: two steps of 2^-23 every 16 rows of at most a run, a rounding per run and part
+    tol = (2.0 ** -22 * (min(rows, 1024) / 16 + 1) * (3 if dtype == "f32" else 1) + (rows / 1024 + 80) * U) * size
+    assert ((got - want).abs() <= tol + U * want.abs()).all()
+    assert rdy.untouched()
