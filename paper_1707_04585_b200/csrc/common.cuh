@@ -7,6 +7,7 @@
 #include <string>
 #include <vector>
 #include "../../include/revnet.h"
+#include "once.cuh"
 
 typedef __nv_bfloat16 bf16;
 
@@ -52,18 +53,10 @@ struct revnet_ctx {
     std::vector<StampRec> stamp_recs;
 };
 
-// Function attributes (the dynamic shared-memory limit) belong to a device, not to the process: each kernel's
-// launcher keeps one of these and sets its attributes the first time it runs on a device.  Setting them twice
-// is harmless, so no lock: two threads that race both set the same value.
-struct OncePerDevice {
-    bool done[64] = {};
-    bool first(int device) {
-        if (device < 0 || device >= 64) return true;
-        if (done[device]) return false;
-        done[device] = true;
-        return true;
-    }
-};
+// Raises the kernels' limit on dynamic shared memory, once per device (false: refused, which the launch's check reports too).
+template <class... K> inline bool shared_limit(OncePerDevice &once, int device, size_t bytes, K... kernels) {
+    return once.ensure(device, [&] { return (... && (cudaFuncSetAttribute(kernels, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess)); });
+}
 
 // A tensor of C = c0 + c1 channels stored as two NHWC tensors: channels [0,c0) in p0 (row
 // stride c0) and [c0,c0+c1) in p1 (row stride c1).  c1 == 0: one plain tensor.

@@ -720,11 +720,7 @@ bool run_fused(Exec &ex, const char *what, int in_mode, const void *in, float in
         if (req.stats) { e.mean = req.stats->mean; e.rstd = req.stats->rstd; }
         if (req.bnbwd) { e.bn = req.bnbwd->bn; e.dgamma = req.bnbwd->dgamma; e.dbeta = req.bnbwd->dbeta; e.coef = req.bnbwd->coef; }
         static OncePerDevice once;
-        if (once.first(ex.ctx->device)) {
-            cudaFuncSetAttribute(conv_fused_kernel<16, 192>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            cudaFuncSetAttribute(conv_fused_kernel<8, 192>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            cudaFuncSetAttribute(conv_fused_kernel<8, 320>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-        }
+        shared_limit(once, ex.ctx->device, 227 * 1024, conv_fused_kernel<16, 192>, conv_fused_kernel<8, 192>, conv_fused_kernel<8, 320>);
         dim3 grid((unsigned)ctas, (unsigned)s.n_tiles);
         launch(ex, s.EW == 16 ? conv_fused_kernel<16, 192> : (s.NBT == 320 ? conv_fused_kernel<8, 320> : conv_fused_kernel<8, 192>), grid, fused_threads(s.EW, s.NBT), s.smem, A);
         const double bytes = (double)geo.P() * cin * (in_mode == kInBf16 ? 2 : (in_mode == kInBwd ? 8 : 4)) + (double)geo.P() * cout * (sign || req.bnbwd ? 8 : 4) +

@@ -306,8 +306,7 @@ template <int WM, int WN, int WK, class AL, class BL, class EP>
 static void launch_tile(Exec &ex, AL al, BL bl, EP ep, int M, int N, int K, int splits, int k_per_split) {
     using T = GemmTile<WM, WN, WK>;
     static OncePerDevice once;
-    if (T::kSmem > 48 * 1024 && once.first(ex.ctx->device))
-        cudaFuncSetAttribute(conv_gemm_kernel<WM, WN, WK, AL, BL, EP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kSmem);
+    if (T::kSmem > 48 * 1024) shared_limit(once, ex.ctx->device, T::kSmem, conv_gemm_kernel<WM, WN, WK, AL, BL, EP>);
     launch(ex, conv_gemm_kernel<WM, WN, WK, AL, BL, EP>, dim3((M + T::BM - 1) / T::BM, (N + T::BN - 1) / T::BN, splits), 256, T::kSmem, al, bl, ep, M, N, K, k_per_split);
 }
 // Tile of a forward / data-gradient GEMM (M = pixels): N tile as wide as the layer up to 64; the tallest M tile that still
@@ -465,7 +464,7 @@ template <class WL, class EP>
 static void launch_direct(Exec &ex, const float *in, WL wl, EP ep, const DirectGeom &g) {
     const int smem = (9 * g.kc * g.CB * 16 + 2 * (g.gx * 4 + 2) * (g.gy * 8 + 2) * g.gi * g.pitch) * 4;      // at most 157 KB
     static OncePerDevice once;
-    if (once.first(ex.ctx->device)) cudaFuncSetAttribute(conv3x3_direct_kernel<WL, EP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    shared_limit(once, ex.ctx->device, 160 * 1024, conv3x3_direct_kernel<WL, EP>);
     const int nbs = (g.Co + g.CB * 16 - 1) / (g.CB * 16);
     int per_sm = 16 / g.NW, fit = 227 * 1024 / (smem + 1024);
     if (per_sm > fit) per_sm = fit;
@@ -838,7 +837,7 @@ void conv_wgrad_simt(Exec &ex, const void *gq, bool g_bf16, const void *a, bool 
         float *part = ctas > 1 ? ex.ws.get<float>((size_t)ctas * Co * KC) : dW;
         if (!ex.dry) {
             static OncePerDevice once;
-            if (once.first(ex.ctx->device)) cudaFuncSetAttribute(wgrad3x3_strip_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+            shared_limit(once, ex.ctx->device, 200 * 1024, wgrad3x3_strip_kernel);
             launch(ex, wgrad3x3_strip_kernel, ctas, threads, smem, (const float *)a, (const float *)gq, part, st);
             ex.check("conv_wgrad_strip", (double)P * (g.Co + g.Ci) * 4 + (double)Co * KC * 4, 2.0 * Co * KC * (double)P);
             if (ctas > 1) {

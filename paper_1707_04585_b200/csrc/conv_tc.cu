@@ -1205,11 +1205,7 @@ bool run_conv_tc(Exec &ex, const char *what, const void *act, Geom gin, int cin,
         if (req.stats) { e.mean = req.stats->mean; e.rstd = req.stats->rstd; }
         if (req.bnbwd) { e.t = req.bnbwd->t; e.bn = req.bnbwd->bn; e.dgamma = req.bnbwd->dgamma; e.dbeta = req.bnbwd->dbeta; e.coef = req.bnbwd->coef; }
         static OncePerDevice once;
-        if (once.first(ex.ctx->device)) {
-            cudaFuncSetAttribute(conv_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            cudaFuncSetAttribute(conv_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            cudaFuncSetAttribute(conv_tc2_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-        }
+        shared_limit(once, ex.ctx->device, 227 * 1024, conv_tc_kernel<true>, conv_tc_kernel<false>, conv_tc2_kernel);
         dim3 grid((unsigned)ctas, (unsigned)s.n_tiles);
         if (pair) launch_cluster(ex, conv_tc2_kernel, grid, 64 + groups * 128, s.smem, 2, map_a, map_b, map_o[0], map_o[1], map_x[0], map_x[1], p);
         else launch(ex, epi_tma ? conv_tc_kernel<true> : conv_tc_kernel<false>, grid, epi_tma ? 64 + groups * 128 : kThreads, s.smem, map_a, map_b, map_o[0], map_o[1], map_x[0], map_x[1], p);
@@ -1279,7 +1275,7 @@ bool run_bn_conv(Exec &ex, Pair t, BnRef bn, Geom gi, const Layer &L, Pair out, 
         if (stats) { e.mean = stats->mean; e.rstd = stats->rstd; }
         q.bn = bn; q.in_q = t.q; q.a_out = a_out; q.P = P; q.raw_stages = raws;
         static OncePerDevice once;
-        if (once.first(ex.ctx->device)) cudaFuncSetAttribute(conv1x1_bn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        shared_limit(once, ex.ctx->device, 227 * 1024, conv1x1_bn_kernel);
         launch(ex, conv1x1_bn_kernel, ctas, kBnThreads, smem, map_raw, map_b, map_o, q);
         ex.check("conv_fprop_bn", (double)P * cin * (a_out ? 6 : 4) + (double)P * cout * 4 + (double)cout * cin * 2, 2.0 * P * cout * cin);
     }
@@ -1907,10 +1903,7 @@ bool conv_wgrad_tc_batch(Exec &ex, int n, const void *const *gq, const void *con
             flops += 2.0 * w[j].go.P() * L[j]->cout * L[j]->cin * p.taps;
         }
         static OncePerDevice once;
-        if (once.first(ex.ctx->device)) {
-            cudaFuncSetAttribute(wgrad_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmemMax);
-            cudaFuncSetAttribute(wgrad_tc2_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWgSmemMax);
-        }
+        shared_limit(once, ex.ctx->device, kWgSmemMax, wgrad_tc_kernel, wgrad_tc2_kernel);
         if (pair) launch_cluster(ex, wgrad_tc2_kernel, (unsigned)cta, kThreads, smem, 2, batch);
         else launch(ex, wgrad_tc_kernel, (unsigned)cta, kThreads, smem, batch);
         ex.check(pair ? "conv_wgrad_tc2" : "conv_wgrad_tc", bytes, flops);

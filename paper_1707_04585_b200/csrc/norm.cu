@@ -384,10 +384,6 @@ Plan plan_of(int rows, const Shape &s, int channels, int row, int full, int byte
 // (shifted rows take more instructions than bytes: as many as fit)
 Plan fwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : (s.most == 512 ? kFwdBytes : kFwdBytes - 1)); }
 Plan bwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : kBwdBytes); }
-template <class K> bool with_shared(Exec &ex, OncePerDevice &once, K kernel, size_t bytes) {
-    if (!once.first(ex.ctx->device)) return true;
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
-}
 // records of dgamma, of the largest grid that a call may have: its rows' alignment decides too
 int parts_of(const revnet_ctx *ctx, const revnet_norm_desc &d) {
     const Shape s = shape_of(d.channels);
@@ -399,7 +395,7 @@ template <int ROWS, class TS, class TB, int CODE, int SLOTS, int THREADS> void f
     constexpr int row = kChunks<TS> + kChunks<TB>;
     constexpr bool async = staged(ROWS, SLOTS, row, THREADS);
     p.stages = fwd_plan(ROWS, s, p.channels, row).stages;
-    if (!with_shared(ex, once, rmsnorm_fwd_kernel<ROWS, TS, TB, CODE, SLOTS, THREADS>, async ? shared_of(1) : 0)) return;
+    if (!shared_limit(once, ex.ctx->device, async ? shared_of(1) : 0, rmsnorm_fwd_kernel<ROWS, TS, TB, CODE, SLOTS, THREADS>)) return;
     launch_stream(ex, bytes, async ? 100 : 0, rmsnorm_fwd_kernel<ROWS, TS, TB, CODE, SLOTS, THREADS>, grid, s.threads, async ? (size_t)p.stages * stage_bytes(ROWS, s, row) : 0, p);
 }
 template <int ROWS, class TS, class TB, int CODE> void fwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {
@@ -413,7 +409,7 @@ template <int ROWS, class TS, class TB, bool FROM_H, int CODE, int SLOTS, int TH
     constexpr bool async = staged(ROWS, SLOTS, row, THREADS);
     p.stages = bwd_plan(ROWS, s, p.channels, row).stages;
     const size_t rows = async ? (size_t)p.stages * stage_bytes(ROWS, s, row) : 0, least = THREADS == 256 ? THREADS * 16 * sizeof(float) : 0, smem = rows > least ? rows : least;
-    if (!with_shared(ex, once, rmsnorm_bwd_kernel<ROWS, TS, TB, FROM_H, CODE, SLOTS, THREADS>, async ? shared_of(1) : least)) return;
+    if (!shared_limit(once, ex.ctx->device, async ? shared_of(1) : least, rmsnorm_bwd_kernel<ROWS, TS, TB, FROM_H, CODE, SLOTS, THREADS>)) return;
     launch_stream(ex, bytes, async ? 100 : 15, rmsnorm_bwd_kernel<ROWS, TS, TB, FROM_H, CODE, SLOTS, THREADS>, grid, s.threads, smem, p);
 }
 template <int ROWS, class TS, class TB, bool FROM_H, int CODE> void bwd_t(Exec &ex, const NormArgs &p, const Shape &s, unsigned grid, double bytes) {

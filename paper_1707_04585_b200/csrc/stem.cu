@@ -434,7 +434,7 @@ template <int COL> static bool fprop_rows(Exec &ex, const float *img, const Stem
     if (smem > 200 * 1024) return false;
     if (ex.dry) return true;
     static OncePerDevice once;
-    if (once.first(ex.ctx->device)) cudaFuncSetAttribute(stem_fprop_row_kernel<COL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    shared_limit(once, ex.ctx->device, 200 * 1024, stem_fprop_row_kernel<COL>);
     const int grid = row_grid(ex, stem_fprop_row_kernel<COL>, T::FW * 32, smem, n_tiles, 1);
     launch(ex, stem_fprop_row_kernel<COL>, grid, T::FW * 32, smem, img, W, out, g, fast_div(g.W * 3), cols, tiles_per_img, n_tiles, cop);
     return true;
@@ -453,7 +453,7 @@ template <int K> static bool wgrad_rows_shape(const StemGeom &g, RowWgrad &w) {
 // part: room for `cap` partials; returns the number written
 template <int K> static int wgrad_rows(Exec &ex, const float *img, const float *gout, const StemGeom &g, const RowWgrad &w, float *part, int cap) {
     static OncePerDevice once;
-    if (once.first(ex.ctx->device)) cudaFuncSetAttribute(stem_wgrad_row_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    shared_limit(once, ex.ctx->device, 200 * 1024, stem_wgrad_row_kernel<K>);
     int parts = row_grid(ex, stem_wgrad_row_kernel<K>, w.nw * 32, w.smem, w.n_tiles, w.blocks_y);
     if (parts > cap) parts = cap;
     launch(ex, stem_wgrad_row_kernel<K>, dim3(parts, w.blocks_y), w.nw * 32, w.smem, img, gout, part, g, fast_div(g.W * 3), w.cols, w.tiles_per_img, w.n_tiles, w.cbw);
@@ -481,10 +481,7 @@ bool stem_fprop(Exec &ex, const float *img, Geom gi, const Layer &L, Pair out) {
     int per_sm = (int)((220 * 1024) / (smem + 1024)); if (per_sm > 8) per_sm = 8; if (per_sm < 1) per_sm = 1;
     int grid = ex.ctx->sm_count * per_sm; if (grid > n_tiles) grid = n_tiles;
     static OncePerDevice once;
-    if (once.first(ex.ctx->device)) {
-        cudaFuncSetAttribute(stem_fprop_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-        cudaFuncSetAttribute(stem_fprop_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    }
+    shared_limit(once, ex.ctx->device, 200 * 1024, stem_fprop_kernel<4>, stem_fprop_kernel<8>);
     if (CO_T == 8) launch(ex, stem_fprop_kernel<8>, grid, 256, smem, img, L.W, out, g, cop, n_tiles);
     else launch(ex, stem_fprop_kernel<4>, grid, 256, smem, img, L.W, out, g, cop, n_tiles);
     ex.check("stem_fprop", (double)g.N * g.H * g.W * g.Ci * 4 + (double)P * g.Co * 4 + (double)g.Co * g.K * 4, 2.0 * P * g.Co * g.K);
@@ -514,10 +511,7 @@ bool stem_wgrad(Exec &ex, const float *img, const float *gout, Geom gi, const La
             if (grid > ex.ctx->sm_count * 2) grid = ex.ctx->sm_count * 2;
             const int S = 256 / G;
             static OncePerDevice once;
-            if (once.first(ex.ctx->device)) {
-                cudaFuncSetAttribute(stem_wgrad_kernel<8, 12>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-                cudaFuncSetAttribute(stem_wgrad_kernel<4, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-            }
+            shared_limit(once, ex.ctx->device, 200 * 1024, stem_wgrad_kernel<8, 12>, stem_wgrad_kernel<4, 4>);
             if (big) launch(ex, stem_wgrad_kernel<8, 12>, grid, 256, smem, img, gout, part, g, cop, kp, n_cg, G, S, n_chunks);
             else launch(ex, stem_wgrad_kernel<4, 4>, grid, 256, smem, img, gout, part, g, cop, kp, n_cg, G, S, n_chunks);
         }

@@ -29,7 +29,8 @@ Exec exec_of(revnet_ctx *ctx, void *stream) {
     ex.ctx = ctx; ex.dry = false; ex.stream = (cudaStream_t)stream;
     return ex;
 }
-int done(const Exec &ex) { return ex.failed ? REVNET_E_CUDA : REVNET_OK; }
+// (a failure is in the context's message: the runtime's record of it would fail the next call too)
+int done(const Exec &ex) { if (ex.failed) cudaGetLastError(); return ex.failed ? REVNET_E_CUDA : REVNET_OK; }
 
 // ---- 8-bit checkpoints
 int check_act8(revnet_ctx *ctx, const revnet_act_desc *in, revnet_act_desc &d) {

@@ -35,7 +35,7 @@ constexpr int kGroups = 6, kGroupWarps = kDecoders / kGroups;    // every kGroup
 constexpr int kRegs = 80, kRegsFew = 40, kRegsSums = 160;        // registers per thread: at launch; then of the control and decoder warps, and of the summing ones
 static_assert((4 + kDecoders) * kRegsFew + kSummers * kRegsSums == kThreads / 32 * kRegs, "the split is the launch's total");
 constexpr int kStep = 64;            // rows per step
-constexpr int kRun = 16;            // steps per run of the tensor cores' own sum
+constexpr int kRun = 16;             // steps per run of the tensor cores' own sum
 constexpr int kM = 256, kN = 256;    // output and input channels of a pair's tile, half of either in each CTA's shared memory
 constexpr int kMaxPairs = 80;
 constexpr int kStepsMin = 8;         // a pair's share of a tile is at least that long: shorter ones do not pay for their sums
@@ -481,7 +481,7 @@ bool encode_2d(void *fn, CUtensorMap *map, CUtensorMapDataType type, const void 
 
 template <int CODE> void run_t(Exec &ex, const Wgrad8Args &a, double bytes, double flops) {
     static OncePerDevice once;
-    if (once.first(ex.ctx->device)) cudaFuncSetAttribute(wgrad8_kernel<CODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (!shared_limit(once, ex.ctx->device, kSmem, wgrad8_kernel<CODE>)) { ex.check("wgrad8"); return; }
     // the split of the registers adds up to what a launch gets with kRegs per thread, no more: a kernel built with fewer would wait for ever
     cudaFuncAttributes attr;
     if (cudaFuncGetAttributes(&attr, wgrad8_kernel<CODE>) != cudaSuccess || attr.numRegs != kRegs) {
@@ -537,7 +537,7 @@ void wgrad8(Exec &ex, const revnet_wgrad_desc &d, const void *dy, const void *ck
     const double bytes = (double)d.rows * (2.0 * d.cout * (w.steps / w.row_steps) + d.cin) + 4.0 * d.cin * d.cout, flops = 2.0 * w.steps * kStep * d.cin * d.cout;
     if (d.code == REVNET_INT8) run_t<REVNET_INT8>(ex, a, bytes, flops);
     else run_t<REVNET_E4M3>(ex, a, bytes, flops);
-    if (w.partial_bytes) {
+    if (w.partial_bytes && !ex.failed) {
         if (w.sharers > 16 * w.rest) sum_t<16, 4>(ex, a);
         else if (w.sharers > 3 * w.rest) sum_t<4, 8>(ex, a);
         else sum_t<1, 32>(ex, a);
