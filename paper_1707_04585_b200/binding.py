@@ -139,16 +139,8 @@ def _stream():
 
 class Context:
     def __init__(self, device: int = 0):
-        global _types, _direct
-        if not _types:
-            import torch
-            _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
-            lib()
-            try:
-                from . import _direct as module          # links to the library above
-                _direct = module
-            except ImportError:
-                pass
+        if device >= 0:                                  # (a planning-only context, -1, needs no torch)
+            _load_types()
         self.h = C.c_void_p()
         self.device = device
         self.home = device if device >= 0 else -2        # where tensors have to be (a CPU tensor calls its place -1)
@@ -472,11 +464,25 @@ def _bad(what, name, why):
     raise e
 
 
-_types = ()             # torch's types by revnet_dtype, then those of flat buffers; filled with the first context, so that importing this module needs no torch
+_types = ()             # torch's types by revnet_dtype, then those of flat buffers; filled with the first context on a device, so that importing this module needs no torch
 F32, BF16, I32, U8 = 0, 1, 2, 3
 # csrc/direct.cpp: the calls below, checks included, at less than half of the host time.  It answers None where it finds anything wrong; then (and
 # without it) the code here checks, and says what.
 _direct = None
+
+
+def _load_types():
+    global _types, _direct
+    if _types:
+        return
+    import torch
+    lib()
+    try:
+        from . import _direct as module                  # links to the library above
+        _direct = module
+    except ImportError:
+        pass
+    _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
 
 
 def _strided(stride, rows, channels, ld):
@@ -487,6 +493,7 @@ def _row_ptr(ctx, what, name, t, rows, channels, ld, dtype):
     """Address of a [rows][channels] tensor (None: null)."""
     if t is None:
         return None
+    _load_types()
     if t.dtype is not _types[dtype] or t.get_device() != ctx.home:
         _bad(what, name, f"must be {_types[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
     if t.shape != (rows, channels) or not ((ld or channels) == channels and t.is_contiguous() or _strided(t.stride(), rows, channels, ld or channels)):
@@ -498,6 +505,7 @@ def _flat_ptr(ctx, what, name, t, n, dtype=F32):
     """Address of n contiguous elements, or of at least n bytes (None: null)."""
     if t is None:
         return None
+    _load_types()
     if t.dtype is not _types[dtype] or t.get_device() != ctx.home or not t.is_contiguous():
         _bad(what, name, f"must be contiguous {_types[dtype]} on cuda:{ctx.device}, got {t.dtype} on {t.device}")
     if t.numel() < n if dtype == U8 else t.numel() != n:
