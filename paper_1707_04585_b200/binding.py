@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import warnings
 from typing import Dict, List
 
 import numpy as np
@@ -471,17 +472,29 @@ F32, BF16, I32, U8 = 0, 1, 2, 3
 _direct = None
 
 
+def _find_direct(torch_version):
+    """The module of the calls without ctypes, if it is there and built for this torch and Python."""
+    from . import build
+    if not os.path.exists(build.DIRECT):
+        return None
+    try:
+        from . import _direct as module                  # links to the library
+        if module.built_for == build.versions(torch_version):
+            return module
+        why = f"it is built for {module.built_for}"
+    except ImportError as e:
+        why = str(e)
+    warnings.warn(f"_direct.so is not used, calls on rows of tokens go through ctypes: {why} (python -m paper_1707_04585_b200.build makes it anew)", RuntimeWarning)
+    return None
+
+
 def _load_types():
     global _types, _direct
     if _types:
         return
     import torch
     lib()
-    try:
-        from . import _direct as module                  # links to the library above
-        _direct = module
-    except ImportError:
-        pass
+    _direct = _find_direct(torch.__version__)
     _types = (torch.float32, torch.bfloat16, torch.int32, torch.uint8)
 
 

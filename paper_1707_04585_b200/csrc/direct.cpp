@@ -177,4 +177,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_direct", nullptr, -1, methods, nu
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__direct() { return PyModule_Create(&module); }
+// built_for: the versions whose headers are in here (build.py); binding.py takes the module for no others
+PyMODINIT_FUNC PyInit__direct() {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", BUILT_FOR)) { Py_DECREF(m); return nullptr; }
+    return m;
+}
