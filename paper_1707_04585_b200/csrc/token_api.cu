@@ -178,8 +178,10 @@ extern "C" int revnet_rmsnorm_bwd(revnet_ctx *ctx, const revnet_norm_desc *desc,
         REFUSE(ck && d.ck_scaled, REVNET_E_INVALID_ARG, "revnet_rmsnorm_bwd: the checkpoint of the backward pass is that of the unscaled rows (ck_scaled = 0)");
         const size_t ss = size_of(d.stream_dtype), sb = size_of(d.branch_dtype);
         REFUSE(!aligned(dn, sb) || !aligned(dr, sb) || !aligned(dh, ss) || !aligned(h, ss) || !aligned(dx, ss) || !aligned(gamma, 4) || !aligned(rstd, 4) ||
-               !aligned(dgamma, 4) || !aligned(ck, 256), REVNET_E_MISALIGNED, "revnet_rmsnorm_bwd: the checkpoint on 256 bytes, tensors on their elements' size");
+               !aligned(ck, 256), REVNET_E_MISALIGNED, "revnet_rmsnorm_bwd: the checkpoint on 256 bytes, tensors on their elements' size");
     }
+    // (dgamma is written without rows too)
+    REFUSE(!aligned(dgamma, 4), REVNET_E_MISALIGNED, "revnet_rmsnorm_bwd: dgamma on its elements' size");
     REFUSE(dgamma && !workspace, REVNET_E_INVALID_ARG, "revnet_rmsnorm_bwd: null workspace");
     REFUSE(dgamma && !aligned(workspace, 16), REVNET_E_MISALIGNED, "revnet_rmsnorm_bwd: the workspace must be 16-byte aligned");
     REFUSE(dgamma && workspace_bytes < rmsnorm_bwd_workspace(ctx, d), REVNET_E_WORKSPACE_TOO_SMALL, "revnet_rmsnorm_bwd: workspace too small");
