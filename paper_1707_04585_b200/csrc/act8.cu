@@ -26,7 +26,8 @@ template <int ACT> __device__ __forceinline__ void act_grad(float x, float &a, f
     else if (ACT == REVNET_ACT_GELU) {
         const float s = sigmoid(gelu_arg(x));
         a = x * s;
-        d = s + a * (1.f - s) * (1.5957691216057308f * (1.f + 0.134145f * x * x));
+        // (x^2 would be infinite from 1.8e19 on; the factor before it is 0 long before 1e30)
+        d = s + a * (1.f - s) * (1.5957691216057308f * (1.f + 0.134145f * fminf(x * x, 1e30f)));
     } else if (ACT == REVNET_ACT_SILU) {
         const float s = sigmoid(x);
         a = x * s;

@@ -242,3 +242,31 @@ def test_weight_gradient_schedules(ctx, rows, cin, cout, waves, cut, crossing, d
     tol = (2.0 ** -22 * (min(rows, 1024) / 16 + 1) * (3 if dtype == "f32" else 1) + (rows / 1024 + 80) * U) * size
     assert ((got - want).abs() <= tol + U * want.abs()).all()
     assert rdy.untouched()
+
+
+# ------------------------------------------------------------------ activations far out
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("kind", ["gelu", "silu", "swiglu", "relu"])
+def test_activations_of_the_largest_values(ctx, kind, code):
+    """Out there an activation is x or 0 and its derivative 1 or 0; sums and products on the way stay finite or their limits are taken."""
+    sizes = [20.0, 1e4, 1e9, 1e13, 1.1e19, 3e19, 1e20, 1e30, 3e38]
+    x = torch.tensor([[s, -s] * 16 for s in sizes])              # one block per row: every value is held to its code's step
+    if kind == "swiglu":
+        x = torch.cat([x, torch.full_like(x, 0.5)], 1)           # gates of all sizes, and what they gate
+    rows, c = x.shape
+    out = c // 2 if kind == "swiglu" else c
+    ck, a = Ck(rows, c), Rows(rows, out, "f32")
+    d = B.act_desc(rows, c, "f32", code, kind)
+    B.revnet_act_store(ctx, d, x.cuda(), ck.t, a.t)
+    x8 = ref.held(ck.t, rows, c, code)
+    first = x[:, :out]
+    up = 0.5 if kind == "swiglu" else 1.0
+    within(a.cpu(), torch.where(first > 0, first.double() * up, 0.0), 2.0 ** -20 * first.double().abs().clamp_max(1e4) * up)      # (20 is not quite there: e^-20 20 = 4e-8)
+    da, dx, ack = torch.full((rows, out), 3.0), Rows(rows, c, "f32"), Ck(rows, out)
+    B.revnet_act_bwd(ctx, d, ck.t, da.cuda(), dx.t, ack.t)
+    g8 = x8[:, :out]
+    within(dx.cpu()[:, :out], torch.where(g8 > 0, 3.0 * up, 0.0).double(), torch.full_like(g8, 2.0 ** -18))
+    if kind == "swiglu":
+        want = torch.where(g8 > 0, 3.0 * g8, 0.0)
+        within(dx.cpu()[:, out:], torch.where(want > torch.finfo(torch.float32).max, math.inf, want), 2.0 ** -20 * g8.abs().clamp_max(1e4))      # (3 * 3e38 is beyond float32)
+    assert torch.isfinite(ref.held(ack.t, rows, out, code)).all()
