@@ -72,7 +72,10 @@ template <int N, int WARPS> __device__ __forceinline__ void row_sum(float (&v)[N
 // Backward, with more reads per write, gains from more: 16384 x 4096 bf16 2 x 2 (80) 90, 2 x 3 (120) 83, 2 x 4 (160) 84; 4096 float32 2 x 2 (144)
 // 138, 2 x 3 (216) 151; 200704 x 512 float32 from h 1 x 3 (144) 238, 2 x 2 (192) 239.  More than three rows never paid.  (With 80 registers, for three
 // CTAs, a float32 stream with a bf16 branch spills: 16384 x 4096 150 against 136.)
-constexpr int kMaxStages = 3, kFwdBytes = 96 * 1024, kBwdBytes = 160 * 1024;
+// The forward's limit is less than 96 KB.  Two rows and three (2^26 values, us): at 96 KB, rows that fill all threads, bf16 4096 102 and 114, 8192 107 both,
+// float32 512 281 and 306; just below it, bf16 4080 109 and 115, 4064 109 and 111, 4032 109 and 111, 1000 115 and 109, 8128 109 and 107, 8064 109 and
+// 105, float32 4064 201 and 195, 2032 201 and 192, 2000 203 and 189; at 90 KB float32 3840 201 and 185.  A limit of 95 KB only moves the step.
+constexpr int kMaxStages = 3, kFwdBytes = 96 * 1024 - 1, kBwdBytes = 160 * 1024;
 __host__ __device__ constexpr int per_sm_of(int threads) { return threads == 512 ? 1 : 2; }        // of the most threads, with 128 registers each
 __host__ __device__ constexpr int shared_of(int per_sm) { return (228 / per_sm - 2) * 1024; }        // bytes of a CTA for stages: an SM has 228 KB, the system takes 1 KB per CTA, the sums less than another
 __host__ __device__ constexpr bool staged(int rows, int slots, int row, int threads) {        // do two stages fit
@@ -154,6 +157,8 @@ __global__ void __launch_bounds__(THREADS, per_sm_of(THREADS)) rmsnorm_fwd_kerne
             if (++stage == p.stages) stage = 0;
         }
         row_sum(sum, tpr, which, half, red);
+        // (rsqrtf is off by two steps at most.  16384 x 4096: 415 of the bf16 outputs and 52 of the codes fall otherwise than exact ones would; with
+        // divisions and roots in float32 throughout 474 and 65)
         const float rstd = rsqrtf(sum[0] * p.inv_c + p.eps);
         if (p.rstd && row_ok && t == 0) p.rstd[row] = rstd;
         if (!p.n && !p.ck.codes) continue;
@@ -382,7 +387,7 @@ Plan plan_of(int rows, const Shape &s, int channels, int row, int full, int byte
     return p;
 }
 // (shifted rows take more instructions than bytes: as many as fit)
-Plan fwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : (s.most == 512 ? kFwdBytes : kFwdBytes - 1)); }
+Plan fwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : kFwdBytes); }
 Plan bwd_plan(int rows, const Shape &s, int channels, int row) { return plan_of(rows, s, channels, row, per_sm_of(s.most), rows == kShifted ? shared_of(1) : kBwdBytes); }
 // records of dgamma, of the largest grid that a call may have: its rows' alignment decides too
 int parts_of(const revnet_ctx *ctx, const revnet_norm_desc &d) {
