@@ -319,7 +319,8 @@ int revnet_train_step_host(revnet_ctx *ctx, revnet_plan *plan,
  *   - Rows are `ld` elements apart, channels contiguous; ld = 0 stands for the row's length.  Rows of 16-byte multiples at 16-byte
  *     addresses take wide accesses; any other stride, length or (element-aligned) address is legal and slower.
  *   - rows = 0 is legal: nothing is read, row outputs stay as they are, gradients of parameters are set to zero.  Row tensors may then be null.
- *   - Elements between a row's end and the next row's start, and rows behind the last one, are neither read nor written.
+ *   - Elements between a row's end and the next row's start are not written, and what lies there changes no result; in front of a row that starts off a
+ *     16-byte boundary up to 15 bytes of them may be read.  Rows behind the last one, and what lies in front of the first, are neither read nor written.
  *   - float32 arithmetic on every type; bf16 outputs are rounded once, at the end.
  *   - The context's device must be the current one.  Results do not depend on timing: no sum is formed by atomics.
  *   - Outputs may alias inputs only where a call says so. */

@@ -235,7 +235,7 @@ template <int ROWS, class T> __device__ __forceinline__ void store16(T *p, int c
 // instruction, and wait for each other (__syncwarp behind the wait) before a thread reads its own 16 channels.  A thread's chunks are
 // neighbours, so eight lanes that read their k-th chunk would meet in half or a quarter of the banks: chunk c lies at c ^ (bits 3.. of c).
 // kShifted: the aligned chunks that hold the channels, one more than their number (which lies behind them as it is); the first may start with
-// the end of the row before, or with what lies between the rows, but with nothing in front of the tensor.
+// up to 15 bytes of the row before, or of what lies between the rows (shifted away), but with nothing in front of the tensor.
 __device__ __forceinline__ void copy16(void *dst, const void *src, int bytes) {       // bytes of src, zeros behind them (0: nothing is read)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes) : "memory");
 }

@@ -270,3 +270,33 @@ def test_activations_of_the_largest_values(ctx, kind, code):
         want = torch.where(g8 > 0, 3.0 * g8, 0.0)
         within(dx.cpu()[:, out:], torch.where(want > torch.finfo(torch.float32).max, math.inf, want), 2.0 ** -20 * g8.abs().clamp_max(1e4))      # (3 * 3e38 is beyond float32)
     assert torch.isfinite(ref.held(ack.t, rows, out, code)).all()
+
+
+# ------------------------------------------------------------------ what lies between rows
+@pytest.mark.parametrize("stream,branch", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("rows,channels,pad,skip", [(300, 45, 2, 1), (700, 1001, 3, 5), (200, 5001, 1, 7), (90, 8203, 5, 3)])
+def test_what_lies_between_rows_changes_nothing(ctx, rows, channels, pad, skip, stream, branch):
+    """Infinities and NaN in front of the first row, between the rows and behind the last one."""
+    x, r, dn, dh = (data(rows, channels, t, i) for i, t in enumerate((stream, branch, branch, stream)))
+    gamma = torch.ones(channels).cuda()
+    got = []
+    for fill in (0.0, math.inf, math.nan):
+        def view(t, dtype):
+            v = Rows(rows, channels, dtype, pad, skip, t)
+            v.buf[v.out] = fill
+            return v
+        vx, vr, vdn, vdh = view(x, stream), view(r, branch), view(dn, branch), view(dh, stream)
+        h, n, ck, rstd = Rows(rows, channels, stream, pad, skip), Rows(rows, channels, branch, pad, skip), Ck(rows, channels), torch.empty(rows, device="cuda")
+        d = B.norm_desc(rows, channels, stream, branch, 1e-5, "int8", False, vx.ld, vr.ld)
+        B.revnet_rmsnorm_fwd(ctx, d, vx.t, vr.t, gamma, h.t, n.t, ck.t, rstd)
+        dx, dg = Rows(rows, channels, stream, pad, skip), torch.empty(channels, device="cuda")
+        ws = torch.empty(B.revnet_rmsnorm_workspace_bytes(ctx, d), dtype=torch.uint8, device="cuda")
+        B.revnet_rmsnorm_bwd(ctx, d, vdn.t, vdh.t, None, ck.t, rstd, gamma, dx.t, None, dg, ws)
+        da, a = Rows(rows, channels, branch, pad, skip), Rows(rows, channels, branch, pad, skip)
+        e = B.act_desc(rows, channels, branch, "int8", "silu", vr.ld, vr.ld)
+        kept = Ck(rows, channels)
+        B.revnet_act_store(ctx, e, vr.t, kept.t, a.t)
+        B.revnet_act_bwd(ctx, e, kept.t, vdn.t, da.t)
+        got.append([t.clone() for t in (h.t, n.t, rstd, dx.t, dg, a.t, da.t)])
+    for other in got[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(got[0], other)) and all(torch.isfinite(p.float()).all() for p in other)
