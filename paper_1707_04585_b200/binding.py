@@ -413,18 +413,28 @@ def revnet_transition_kept_bytes(ctx, desc):
     return k.value, w.value
 
 
+def _kept_ptr(ctx, what, kept, need):
+    """Address of the buffer that keeps a layer's input (of any type)."""
+    if kept is None:
+        _bad(what, "kept", "is missing")
+    at, size = _ws(ctx, what, kept, "kept")
+    if size < need:
+        _bad(what, "kept", f"must hold {need} bytes, got {size}")
+    return C.c_void_p(at)
+
+
 def revnet_transition_keep(ctx, desc, in1, in2, code, kept):
-    if kept.numel() * kept.element_size() < revnet_transition_kept_bytes(ctx, desc)[0]:
-        _bad("revnet_transition_keep", "kept", "is too small")
-    ctx.check(lib().revnet_transition_keep(ctx.h, C.byref(desc), _ptr(in1), _ptr(in2), C.c_int(CODE[code]), _ptr(kept), _stream()), "revnet_transition_keep")
+    w = "revnet_transition_keep"
+    at = _kept_ptr(ctx, w, kept, revnet_transition_kept_bytes(ctx, desc)[0])
+    ctx.check(lib().revnet_transition_keep(ctx.h, C.byref(desc), _ptr(in1), _ptr(in2), C.c_int(CODE[code]), at, _stream()), w)
 
 
 def revnet_transition_bwd_kept(ctx, desc, code, kept, dout1, dout2, W, gamma, beta, din1, din2, dW, dgamma, dbeta, workspace):
-    if kept.numel() * kept.element_size() < revnet_transition_kept_bytes(ctx, desc)[0]:
-        _bad("revnet_transition_bwd_kept", "kept", "is too small")
-    ctx.check(lib().revnet_transition_bwd_kept(ctx.h, C.byref(desc), C.c_int(CODE[code]), _ptr(kept), _ptr(dout1), _ptr(dout2), _ptr(W), _ptr(gamma),
+    w = "revnet_transition_bwd_kept"
+    at = _kept_ptr(ctx, w, kept, revnet_transition_kept_bytes(ctx, desc)[0])
+    ctx.check(lib().revnet_transition_bwd_kept(ctx.h, C.byref(desc), C.c_int(CODE[code]), at, _ptr(dout1), _ptr(dout2), _ptr(W), _ptr(gamma),
                                                _ptr(beta), _ptr(din1), _ptr(din2), _ptr(dW), _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
-                                               _nbytes(workspace), _stream()), "revnet_transition_bwd_kept")
+                                               _nbytes(workspace), _stream()), w)
 
 
 def revnet_block_fwd_noalloc(ctx, desc, x1, x2, F, G, y1, y2):
@@ -534,12 +544,12 @@ def _ck_ptr(ctx, what, name, t, rows, channels):
     return None if t is None else _flat_ptr(ctx, what, name, t, _ck_bytes(rows, channels), U8)
 
 
-def _ws(ctx, what, t):
+def _ws(ctx, what, t, name="workspace"):
     """Address and size of a workspace (None: null, 0)."""
     if t is None:
         return None, 0
     if t.get_device() != ctx.home or not t.is_contiguous():
-        _bad(what, "workspace", f"must be contiguous on cuda:{ctx.device}, got one on {t.device}")
+        _bad(what, name, f"must be contiguous on cuda:{ctx.device}, got one on {t.device}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 

@@ -387,6 +387,7 @@ extern "C" int revnet_transition_keep(revnet_ctx *ctx, const revnet_transition_d
     if (rc) return rc;
     if (!in1 || (d->in_split && !in2) || !kept || (code != REVNET_INT8 && code != REVNET_E4M3)) return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_keep: null pointer or unknown code");
     if (!aligned16({in1, in2}) || ((uintptr_t)kept & 255)) return fail(ctx, REVNET_E_MISALIGNED, "revnet_transition_keep: inputs must be 16-byte, the buffer 256-byte aligned");
+    if (!device_is_current(ctx)) return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_keep: the context's device must be current");
     Exec ex = trans_exec(ctx, d, false, nullptr, 0, stream);
     for (int i = 0; i < kept_parts(d); i++)
         act8_store(ex, kept_act(d, code), i ? in2 : in1, (char *)kept + i * kept_part_bytes(d), nullptr, d->in_split ? ex.q : 0.f);
@@ -410,6 +411,7 @@ extern "C" int revnet_transition_bwd_kept(revnet_ctx *ctx, const revnet_transiti
         return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_bwd_kept: null pointer");
     if (!aligned16({dout1, dout2, W, gamma, beta, din1, din2, dW, dgamma, dbeta}))
         return fail(ctx, REVNET_E_MISALIGNED, "revnet_transition_bwd_kept: pointers must be 16-byte aligned");
+    if (!device_is_current(ctx)) return fail(ctx, REVNET_E_INVALID_ARG, "revnet_transition_bwd_kept: the context's device must be current");
     Exec ex = trans_exec(ctx, &f, false, nullptr, 0, stream);
     for (int i = 0; i < kept_parts(d); i++)
         act8_load(ex, kept_act(d, code), (const char *)kept + i * kept_part_bytes(d), i ? in2 : in1);

@@ -27,6 +27,14 @@ static inline int row_access(const void *p, int64_t ld, int size, int channels) 
     return a % 16 || channels * size % 16 ? 0 : (a % 32 ? 1 : 2);
 }
 
+// The context's device has to be current: its kernels and their parameters belong to it.
+static inline bool device_is_current(const revnet_ctx *ctx) {
+    int dev = -1;
+    if (ctx->device >= 0 && cudaGetDevice(&dev) == cudaSuccess && dev == ctx->device) return true;
+    cudaGetLastError();
+    return false;
+}
+
 // ---------------------------------------------------------------- act8.cu, norm.cu, wgrad8.cu, logprobs.cu
 // q not 0: x is int32 fixed point with that step (float32 descriptor, a null)
 void act8_store(Exec &ex, const revnet_act_desc &d, const void *x, void *ck, void *a, float q = 0.f);

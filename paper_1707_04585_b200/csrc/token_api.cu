@@ -15,15 +15,7 @@ int size_of(int t) { return t == REVNET_F32 ? 4 : 2; }
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
-// The context's device has to be current: its kernels and their parameters belong to it.
-int check_device(revnet_ctx *ctx, const char *who) {
-    int dev = -1;
-    if (ctx->device < 0 || cudaGetDevice(&dev) != cudaSuccess || dev != ctx->device) {
-        cudaGetLastError();
-        return fail(ctx, REVNET_E_INVALID_ARG, who);
-    }
-    return REVNET_OK;
-}
+int check_device(revnet_ctx *ctx, const char *who) { return device_is_current(ctx) ? REVNET_OK : fail(ctx, REVNET_E_INVALID_ARG, who); }
 Exec exec_of(revnet_ctx *ctx, void *stream) {
     Exec ex;
     ex.ctx = ctx; ex.dry = false; ex.stream = (cudaStream_t)stream;
