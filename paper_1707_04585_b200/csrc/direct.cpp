@@ -78,6 +78,15 @@ struct Call {
     }
 };
 
+// Python's lock is given back for the entry point itself, as ctypes does: a launch waits while its stream's queue is full, perhaps for a host function
+// that a Python thread has to run.  Made behind the last look at a Python object.
+struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked &) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // (the operands in the binding's order)
 template <class F> PyObject *guarded(F &&f) {
     int status;
@@ -96,7 +105,9 @@ PyObject *act_store(PyObject *, PyObject *const *args, Py_ssize_t n) {
         Call c(args, n, 3, "ActDesc", sizeof(revnet_act_desc));
         const auto &d = c.desc<revnet_act_desc>();
         void *x = c.rows(d.rows, d.channels, d.ld_x, d.dtype), *ck = c.checkpoint(d.rows, d.channels), *a = c.rows(d.rows, a_channels(d), d.ld_a, d.dtype);
-        return revnet_act_store(c.ctx, &d, x, ck, a, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_act_store(c.ctx, &d, x, ck, a, stream);
     });
 }
 PyObject *act_load(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -104,7 +115,9 @@ PyObject *act_load(PyObject *, PyObject *const *args, Py_ssize_t n) {
         Call c(args, n, 2, "ActDesc", sizeof(revnet_act_desc));
         const auto &d = c.desc<revnet_act_desc>();
         void *ck = c.checkpoint(d.rows, d.channels), *a = c.rows(d.rows, a_channels(d), d.ld_a, d.dtype);
-        return revnet_act_load(c.ctx, &d, ck, a, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_act_load(c.ctx, &d, ck, a, stream);
     });
 }
 PyObject *act_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -113,7 +126,9 @@ PyObject *act_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const auto &d = c.desc<revnet_act_desc>();
         void *ck = c.checkpoint(d.rows, d.channels), *da = c.rows(d.rows, a_channels(d), d.ld_a, d.dtype), *dx = c.rows(d.rows, d.channels, d.ld_x, d.dtype);
         void *a_ck = c.checkpoint(d.rows, a_channels(d));
-        return revnet_act_bwd(c.ctx, &d, ck, da, dx, a_ck, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_act_bwd(c.ctx, &d, ck, da, dx, a_ck, stream);
     });
 }
 PyObject *rmsnorm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -124,7 +139,9 @@ PyObject *rmsnorm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
         auto branch_row = [&] { return c.rows(d.rows, d.channels, d.ld_branch, d.branch_dtype); };
         void *x = stream_row(), *r = branch_row(), *gamma = c.flat(d.channels), *h = stream_row(), *out = branch_row(), *ck = c.checkpoint(d.rows, d.channels);
         void *rstd = c.flat(d.rows);
-        return revnet_rmsnorm_fwd(c.ctx, &d, x, r, (const float *)gamma, h, out, ck, (float *)rstd, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_rmsnorm_fwd(c.ctx, &d, x, r, (const float *)gamma, h, out, ck, (float *)rstd, stream);
     });
 }
 PyObject *rmsnorm_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -137,7 +154,9 @@ PyObject *rmsnorm_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
         void *dx = stream_row(), *dr = branch_row(), *dgamma = c.flat(d.channels);
         size_t bytes;
         void *ws = c.workspace(bytes);
-        return revnet_rmsnorm_bwd(c.ctx, &d, dn, dh, h, ck, (const float *)rstd, (const float *)gamma, dx, dr, (float *)dgamma, ws, bytes, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_rmsnorm_bwd(c.ctx, &d, dn, dh, h, ck, (const float *)rstd, (const float *)gamma, dx, dr, (float *)dgamma, ws, bytes, stream);
     });
 }
 PyObject *linear_wgrad(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -147,7 +166,9 @@ PyObject *linear_wgrad(PyObject *, PyObject *const *args, Py_ssize_t n) {
         void *dy = c.rows(d.rows, d.cout, d.ld_dy, d.dy_dtype), *ck = c.checkpoint(d.rows, d.cin), *gamma = c.flat(d.cin), *dW = c.flat((int64_t)d.cin * d.cout);
         size_t bytes;
         void *ws = c.workspace(bytes);
-        return revnet_linear_wgrad(c.ctx, &d, dy, ck, (const float *)gamma, (float *)dW, ws, bytes, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_linear_wgrad(c.ctx, &d, dy, ck, (const float *)gamma, (float *)dW, ws, bytes, stream);
     });
 }
 PyObject *logprobs_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -156,7 +177,9 @@ PyObject *logprobs_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const auto &d = c.desc<revnet_logprob_desc>();
         void *logits = c.rows(d.rows, d.vocab, d.ld, d.dtype), *targets = c.flat(d.rows, at::kInt), *logp = c.flat(d.rows), *entropy = c.flat(d.rows);
         void *lse = c.flat(d.rows), *top = c.flat(d.rows * d.k), *index = c.flat(d.rows * d.k, at::kInt);
-        return revnet_logprobs_fwd(c.ctx, &d, logits, (const int32_t *)targets, (float *)logp, (float *)entropy, (float *)lse, (float *)top, (int32_t *)index, c.stream());
+        void *const stream = c.stream();
+        Unlocked u;
+        return revnet_logprobs_fwd(c.ctx, &d, logits, (const int32_t *)targets, (float *)logp, (float *)entropy, (float *)lse, (float *)top, (int32_t *)index, stream);
     });
 }
 PyObject *logprobs_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -165,8 +188,10 @@ PyObject *logprobs_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
         const auto &d = c.desc<revnet_logprob_desc>();
         void *logits = c.rows(d.rows, d.vocab, d.ld, d.dtype), *targets = c.flat(d.rows, at::kInt), *lse = c.flat(d.rows), *entropy = c.flat(d.rows);
         void *dlogp = c.flat(d.rows), *dentropy = c.flat(d.rows), *dlogits = c.rows(d.rows, d.vocab, d.ld, d.dtype);
+        void *const stream = c.stream();
+        Unlocked u;
         return revnet_logprobs_bwd(c.ctx, &d, logits, (const int32_t *)targets, (const float *)lse, (const float *)entropy, (const float *)dlogp, (const float *)dentropy,
-                                   dlogits, c.stream());
+                                   dlogits, stream);
     });
 }
 

@@ -102,3 +102,36 @@ def test_both_ways_refuse_the_same_tensors(ctx, entry, monkeypatch):
             m.setattr(B, "_direct", None)
             checked(ctx, desc, *put.values())
     torch.cuda.synchronize()
+
+
+def test_other_threads_run_while_a_launch_waits_for_the_queue(ctx):
+    """A stream takes so many launches ahead; the next one waits.  That must not hold up Python's other threads: a host function in front of it in the stream
+    may need one."""
+    import threading
+    import time
+    desc, args = calls(ctx)["act_load"]
+    B.revnet_act_load(ctx, desc, *args.values())
+    torch.cuda.synchronize()
+    gaps, stop = [0.0], threading.Event()
+
+    def beat():
+        last = time.perf_counter()
+        while not stop.is_set():
+            time.sleep(0.001)
+            now = time.perf_counter()
+            gaps.append(now - last)
+            last = now
+    t = threading.Thread(target=beat)
+    t.start()
+    try:
+        torch.cuda._sleep(2_500_000_000)             # clocks: more than a second of nothing
+        begin = time.perf_counter()
+        for _ in range(5000):
+            B.revnet_act_load(ctx, desc, *args.values())
+        waited = time.perf_counter() - begin
+    finally:
+        stop.set()
+        t.join()
+        torch.cuda.synchronize()
+    assert waited > 0.5              # the launches did wait
+    assert max(gaps) < 0.3
