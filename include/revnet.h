@@ -362,7 +362,8 @@ int revnet_act_load(revnet_ctx *ctx, const revnet_act_desc *desc, const void *ck
 int revnet_act_bwd(revnet_ctx *ctx, const revnet_act_desc *desc, const void *ck, const void *da, void *dx, void *a_ck, void *stream);
 
 /* Root-mean-square norm behind the residual's addition (the coupling y = x + F of Section 3.1, then the next function's norm):
- *   h = x + r rounded to the stream's type, rstd = 1 / sqrt(mean(h^2) + eps), xh = h * rstd, n = xh * gamma. */
+ *   h = x + r rounded to the stream's type, rstd = 1 / sqrt(mean(h^2) + eps), xh = h * rstd, n = xh * gamma.
+ * The sum of the squares is a float32: where it is beyond 3.4e38 (one |h| above 1.8e19 will do) rstd is 0. */
 typedef struct {
     int64_t rows;            /* < 2^31 */
     int channels;            /* 1 .. 16384 */

@@ -300,3 +300,17 @@ def test_what_lies_between_rows_changes_nothing(ctx, rows, channels, pad, skip, 
         got.append([t.clone() for t in (h.t, n.t, rstd, dx.t, dg, a.t, da.t)])
     for other in got[1:]:
         assert all(torch.equal(p, q) for p, q in zip(got[0], other)) and all(torch.isfinite(p.float()).all() for p in other)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_whose_squares_leave_the_range_of_float32(ctx, dtype):
+    """Such a row has rstd 0, and nothing of it is kept; the others are as ever."""
+    x = data(4, 300, dtype, 30)
+    x[1], x[2, 7] = 1e19, -3e38
+    n, rstd, ck = Rows(4, 300, dtype), torch.empty(4, device="cuda"), Ck(4, 300)
+    B.revnet_rmsnorm_fwd(ctx, B.norm_desc(4, 300, dtype, dtype), x.cuda(), None, None, None, n.t, ck.t, rstd)
+    want, _, wn = ref.norm_fwd(x.double(), 1.0, 1e-5)
+    assert (rstd[1:3] == 0).all() and (n.t[1:3] == 0).all() and (ref.held(ck.t, 4, 300, "int8")[1:3] == 0).all()
+    for i in (0, 3):
+        within(rstd.cpu().double()[i:i + 1], want[i:i + 1], 64 * U * want[i:i + 1])
+        within(n.cpu()[i], wn[i], 67 * U * wn[i].abs(), dtype)
